@@ -516,6 +516,101 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
                             void* dx, float* dw_f, float* db_f, void* workspace,
                             size_t workspace_bytes, int B, int L, int H, int M, hipStream_t stream);
 
+/*
+ * A paged key/value cache for serving, with grouped heads: query head h reads key head
+ * h / (H / H_kv) and has its own forget gate.
+ *
+ *   format      FOX_CACHE_BF16, or FOX_CACHE_E4M3: each row of d codes with one scale, a
+ *               power of two 2^(exp - 127) chosen from the row's largest magnitude (the
+ *               least that brings it to 448 or below, from 2^-126), so that every value is
+ *               the nearest code times the scale, ties to even, and exact in bf16
+ *   k, v        [n_pages, H_kv, page, d]  of the format's type
+ *   k_exp,v_exp [n_pages, H_kv, page]     uint8, the rows' exp (E4M3 only, else NULL)
+ *   c           [n_pages, H, page]        fp32, the running sum of log f
+ *   page_table  [B, max_pages]            int32; position t of sequence b is slot t % page
+ *               of page page_table[b, t / page].  A number outside [0, n_pages) stands for
+ *               no page: nothing is written there, and its tokens are not attended to.
+ *               Sequences may share pages that are only read.
+ *   page        16, 32, 64, 128 or 256;  d 64 or 128;  H a multiple of H_kv
+ *
+ * The cache is the caller's memory.  Slots that hold no token may hold anything.  The calls
+ * take the number of tokens that each sequence has, seq_len [B] int32 on the device, and do
+ * not change it; what lies past max_pages * page tokens is dropped.
+ */
+typedef enum {
+  FOX_CACHE_BF16 = 0,
+  FOX_CACHE_E4M3 = 1,
+  FOX_CACHE_FORMAT_MAX_ENUM = 0x7FFFFFFF /* not a format: keeps the enum int-sized */
+} fox_cache_format_t;
+
+typedef struct {
+  fox_cache_format_t format;
+  int n_pages, page, max_pages;
+  int B, H, H_kv, d;
+  void* k;
+  void* v;
+  unsigned char* k_exp;
+  unsigned char* v_exp;
+  float* c;
+  const int* page_table;
+} fox_cache_t;
+
+/*
+ * fox_cache_append: writes n new tokens of each sequence (1 <= n <= 64) behind its seq_len[b]
+ *   cached ones.
+ *     k, v        [B,H_kv,n,d] dtype in   (fp32 is rounded once, to the cache's type)
+ *     gate_logit  [B,H,n]      fp32 in
+ *     parent      [B,n] int32  in   the new token that a new token follows, less than its own
+ *                 number; negative (or not less): the last cached token.  NULL: a chain.
+ *     n_new       [B]   int32  in   how many of the n a sequence has; NULL: all
+ *   c of a token is c of the token that it follows plus log sigmoid(gate_logit).  Values that
+ *   are not finite become NaN in an E4M3 cache and do not take part in the row's scale.
+ * fox_cache_append_packed: writes whole prompts, packed as for fox_attn_fwd_packed, behind
+ *   the seq_len[b] cached tokens (NULL: into empty caches).  c [H,N] fp32 comes from
+ *   fox_gate_prefix_packed; a cached sequence's last c is added to it.
+ *     k, v [H_kv,N,d] dtype in;  cu_seqlens [B+1] int32 in
+ * fox_cache_keep: moves token seq_len[b] + index[b,j] to place seq_len[b] + j, for j below
+ *   n_keep[b] (at most n, n <= 64; indexes 0..63): the accepted path of a tree of drafts.
+ *   Everything is read before it is written, so any indexes may be given.  The caller then
+ *   adds n_keep to seq_len.
+ *     index [B,n] int32 in;  n_keep [B] int32 in
+ * fox_cache_read: positions start[b] + t, t < T, below seq_len[b], as dtype: k, v
+ *   [B,H_kv,T,d], c [B,H,T] fp32 (may be NULL); start may be NULL (0).  Other rows of the
+ *   outputs are left as they were.
+ */
+fox_status_t fox_cache_append(const fox_cache_t* cache, fox_dtype_t dtype, const void* k, const void* v,
+                     const float* gate_logit, const int* seq_len, const int* parent,
+                     const int* n_new, int n, hipStream_t stream);
+fox_status_t fox_cache_append_packed(const fox_cache_t* cache, fox_dtype_t dtype, const void* k,
+                            const void* v, const float* c, const int* cu_seqlens,
+                            const int* seq_len, int N, hipStream_t stream);
+fox_status_t fox_cache_keep(const fox_cache_t* cache, const int* seq_len, const int* index,
+                   const int* n_keep, int n, hipStream_t stream);
+fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const int* start,
+                   const int* seq_len, void* k, void* v, float* c, int T, hipStream_t stream);
+
+/*
+ * Attention of n new tokens of each sequence (1 <= n <= 64) over the cache that holds them
+ * already, at places seq_len[b] .. seq_len[b] + n - 1 (fox_cache_append): each attends to the
+ * seq_len[b] tokens before them and, among the new ones, to its ancestors and itself.  n = 1
+ * is a decode step.
+ *
+ *   q       [B,H,n,d] bf16 in      parent, n_new as given to fox_cache_append
+ *   o       [B,H,n,d] bf16 out     lse [B,H,n] fp32 out, as fox_attn_fwd's
+ *           rows of tokens that a sequence does not have (n_new) are left as they were; a
+ *           token whose own place is not in the cache gets o = 0 and lse = -inf
+ *   max_len the most tokens that a sequence has, new ones included: the keys are split for
+ *           it.  Longer sequences are right too, only slower.  0: max_pages * page.
+ *   workspace  at least fox_attn_cache_workspace_bytes() for the same n and max_len (which
+ *           may be 0: then workspace may be NULL)
+ * k and v of the tokens in the cache must be finite.  The order of the sums depends on the
+ * shape and on max_len, not on what other sequences hold.
+ */
+size_t fox_attn_cache_workspace_bytes(const fox_cache_t* cache, int n, int max_len);
+fox_status_t fox_attn_cache(const fox_cache_t* cache, const void* q, const int* seq_len,
+                   const int* parent, const int* n_new, void* o, float* lse, void* workspace,
+                   size_t workspace_bytes, int n, int max_len, float scale, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,6 +26,10 @@ from ._lib import (  # noqa: F401
     EXPORTED,
 )
 
+from ._cache import (  # noqa: E402,F401
+    PagedCache, fox_cache_append, fox_cache_append_packed, fox_cache_keep, fox_cache_read,
+    fox_attn_cache, fox_attn_cache_workspace_bytes,
+)
 from .autograd import (  # noqa: E402,F401
     ForgettingAttention, GateProjection, forget_gate_logits, forgetting_attention,
 )
@@ -51,4 +55,6 @@ __all__ = [
     "fox_attn_bwd_skip_stored", "fox_attn_bwd_fixed_gate_stored",
     "fox_attn_bwd_fixed_gate_stored_workspace_bytes", "fox_attn_bwd_fixed_gate_skip_stored",
     "fox_gate_projection", "fox_gate_projection_bwd", "fox_gate_projection_bwd_workspace_bytes",
+    "PagedCache", "fox_cache_append", "fox_cache_append_packed", "fox_cache_keep",
+    "fox_cache_read", "fox_attn_cache", "fox_attn_cache_workspace_bytes",
 ]

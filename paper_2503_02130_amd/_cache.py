@@ -1,0 +1,216 @@
+"""ctypes binding of the paged key/value cache and the attention over it: argument
+marshalling only, as in _lib.py."""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import torch
+
+from ._lib import (_DT, _check, _on_device, _ptr, _raise, _raw_stream, _workspace, default_scale,
+                   load)
+
+FOX_CACHE_BF16 = 0
+FOX_CACHE_E4M3 = 1
+_FORMATS = {torch.bfloat16: FOX_CACHE_BF16, torch.float8_e4m3fn: FOX_CACHE_E4M3}
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int), ("n_pages", ctypes.c_int), ("page", ctypes.c_int),
+                ("max_pages", ctypes.c_int), ("B", ctypes.c_int), ("H", ctypes.c_int),
+                ("H_kv", ctypes.c_int), ("d", ctypes.c_int), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("c", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class PagedCache:
+    """A paged key/value cache over the caller's tensors (fox_cache_t).
+
+    k, v: [n_pages, H_kv, page, d], torch.float8_e4m3fn (quantised) or torch.bfloat16;
+    k_exp, v_exp: [n_pages, H_kv, page] uint8, the scales 2^(exp - 127) of quantised rows;
+    c: [n_pages, H, page] fp32, the running sum of log f; page_table: [B, max_pages] int32.
+    page is 16, 32, 64, 128 or 256.  The tensors are kept and checked once, here; what they
+    hold, the page table too, may change between calls."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, c: torch.Tensor,
+                 page_table: torch.Tensor, k_exp: Optional[torch.Tensor] = None,
+                 v_exp: Optional[torch.Tensor] = None):
+        if k.dtype not in _FORMATS:
+            raise ValueError(f"unsupported cache dtype {k.dtype}")
+        n_pages, Hkv, page, d = k.shape
+        H, (B, max_pages) = c.shape[1], page_table.shape
+        dev = k.device
+        _check(k, "k", (n_pages, Hkv, page, d), k.dtype, None)
+        _check(v, "v", (n_pages, Hkv, page, d), k.dtype, dev)
+        _check(c, "c", (n_pages, H, page), torch.float32, dev)
+        _check(page_table, "page_table", (B, max_pages), torch.int32, dev)
+        f8 = k.dtype == torch.float8_e4m3fn
+        for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+            if f8:
+                _check(t, name, (n_pages, Hkv, page), torch.uint8, dev)
+            elif t is not None:
+                raise ValueError(f"{name} belongs to a float8_e4m3fn cache")
+        self.k, self.v, self.c, self.page_table = k, v, c, page_table
+        self.k_exp, self.v_exp = k_exp, v_exp
+        self.dtype, self.device = k.dtype, dev
+        self.n_pages, self.page, self.max_pages = n_pages, page, max_pages
+        self.B, self.H, self.H_kv, self.d = B, H, Hkv, d
+        self._struct = _CacheStruct(_FORMATS[k.dtype], n_pages, page, max_pages, B, H, Hkv, d,
+                                    _ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), _ptr(c),
+                                    _ptr(page_table))
+        self._ref = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, page_table: torch.Tensor, n_pages: int, heads: int, kv_heads: int, d: int,
+              page: int = 64, dtype: torch.dtype = torch.float8_e4m3fn) -> "PagedCache":
+        """A cache of n_pages pages on page_table's device, its slots uninitialised."""
+        dev = page_table.device
+        shape = (n_pages, kv_heads, page, d)
+        exps = ([torch.empty(shape[:3], device=dev, dtype=torch.uint8) for _ in range(2)]
+                if dtype == torch.float8_e4m3fn else (None, None))
+        return cls(torch.empty(shape, device=dev, dtype=dtype),
+                   torch.empty(shape, device=dev, dtype=dtype),
+                   torch.empty((n_pages, heads, page), device=dev, dtype=torch.float32),
+                   page_table, *exps)
+
+
+def _check_lens(t: Optional[torch.Tensor], name: str, B: int, device):
+    if t is not None:
+        _check(t, name, (B,), torch.int32, device)
+
+
+def fox_cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
+                     gate_logit: torch.Tensor, seq_len: torch.Tensor,
+                     parent: Optional[torch.Tensor] = None,
+                     n_new: Optional[torch.Tensor] = None) -> None:
+    """Writes n <= 64 new tokens of each sequence, a chain or (parent [B,n] int32) a tree,
+    behind its seq_len [B] int32 cached ones.  k, v [B,H_kv,n,d] bf16 or fp32, gate_logit
+    [B,H,n] fp32; n_new [B] int32: how many of the n a sequence has."""
+    n, dt, dev = k.shape[2], k.dtype, cache.device
+    if dt not in _DT:
+        raise ValueError(f"unsupported dtype {dt}")
+    _check(k, "k", (cache.B, cache.H_kv, n, cache.d), dt, dev)
+    _check(v, "v", (cache.B, cache.H_kv, n, cache.d), dt, dev)
+    _check(gate_logit, "gate_logit", (cache.B, cache.H, n), torch.float32, dev)
+    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    if parent is not None:
+        _check(parent, "parent", (cache.B, n), torch.int32, dev)
+    _check_lens(n_new, "n_new", cache.B, dev)
+    with _on_device(dev):
+        st = load().fox_cache_append(cache._ref, _DT[dt], _ptr(k), _ptr(v), _ptr(gate_logit),
+                                     _ptr(seq_len), _ptr(parent), _ptr(n_new), n,
+                                     _raw_stream(dev.index))
+    _raise(st, "fox_cache_append")
+
+
+def fox_cache_append_packed(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
+                            c: torch.Tensor, cu_seqlens: torch.Tensor,
+                            seq_len: Optional[torch.Tensor] = None) -> None:
+    """Writes whole prompts, packed (k, v [H_kv,N,d] bf16 or fp32, c [H,N] fp32 from
+    fox_gate_prefix_packed, cu_seqlens [B+1] int32), behind the seq_len [B] int32 cached
+    tokens of each sequence (None: none)."""
+    N, dt, dev = k.shape[1], k.dtype, cache.device
+    if dt not in _DT:
+        raise ValueError(f"unsupported dtype {dt}")
+    _check(k, "k", (cache.H_kv, N, cache.d), dt, dev)
+    _check(v, "v", (cache.H_kv, N, cache.d), dt, dev)
+    _check(c, "c", (cache.H, N), torch.float32, dev)
+    _check(cu_seqlens, "cu_seqlens", (cache.B + 1,), torch.int32, dev)
+    _check_lens(seq_len, "seq_len", cache.B, dev)
+    with _on_device(dev):
+        st = load().fox_cache_append_packed(cache._ref, _DT[dt], _ptr(k), _ptr(v), _ptr(c),
+                                            _ptr(cu_seqlens), _ptr(seq_len), N,
+                                            _raw_stream(dev.index))
+    _raise(st, "fox_cache_append_packed")
+
+
+def fox_cache_keep(cache: PagedCache, seq_len: torch.Tensor, index: torch.Tensor,
+                   n_keep: torch.Tensor) -> None:
+    """Moves new token index[b, j] to place j behind seq_len[b], for j < n_keep[b]: the
+    accepted path of a tree of drafts.  index [B,n] (n <= 64), n_keep [B] int32.  seq_len is
+    left to the caller, who adds n_keep to it."""
+    n, dev = index.shape[1], cache.device
+    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    _check(index, "index", (cache.B, n), torch.int32, dev)
+    _check(n_keep, "n_keep", (cache.B,), torch.int32, dev)
+    with _on_device(dev):
+        st = load().fox_cache_keep(cache._ref, _ptr(seq_len), _ptr(index), _ptr(n_keep), n,
+                                   _raw_stream(dev.index))
+    _raise(st, "fox_cache_keep")
+
+
+def fox_cache_read(cache: PagedCache, seq_len: torch.Tensor, T: int,
+                   start: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                   k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                   c: Optional[torch.Tensor] = None
+                   ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Positions start[b] + t, t < T, below seq_len[b], as (k, v [B,H_kv,T,d], c [B,H,T]
+    fp32).  Rows without a token keep what k, v, c held (given: theirs; else zeros)."""
+    dev = cache.device
+    if k is not None:
+        dtype = k.dtype
+    if dtype not in _DT:
+        raise ValueError(f"unsupported dtype {dtype}")
+    shape = (cache.B, cache.H_kv, T, cache.d)
+    k = torch.zeros(shape, device=dev, dtype=dtype) if k is None else k
+    v = torch.zeros(shape, device=dev, dtype=dtype) if v is None else v
+    c = torch.zeros((cache.B, cache.H, T), device=dev) if c is None else c
+    _check(k, "k", shape, dtype, dev)
+    _check(v, "v", shape, dtype, dev)
+    _check(c, "c", (cache.B, cache.H, T), torch.float32, dev)
+    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    _check_lens(start, "start", cache.B, dev)
+    with _on_device(dev):
+        st = load().fox_cache_read(cache._ref, _DT[dtype], _ptr(start), _ptr(seq_len), _ptr(k),
+                                   _ptr(v), _ptr(c), T, _raw_stream(dev.index))
+    _raise(st, "fox_cache_read")
+    return k, v, c
+
+
+def fox_attn_cache_workspace_bytes(cache: PagedCache, n: int, max_len: int = 0) -> int:
+    return int(load().fox_attn_cache_workspace_bytes(cache._ref, n, max_len))
+
+
+def fox_attn_cache(q: torch.Tensor, cache: PagedCache, seq_len: torch.Tensor,
+                   parent: Optional[torch.Tensor] = None, n_new: Optional[torch.Tensor] = None,
+                   max_len: int = 0, scale: Optional[float] = None,
+                   o: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None
+                   ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """O [B,H,n,d] bf16 and LSE [B,H,n] fp32 of the n <= 64 newest tokens of each sequence
+    (at places seq_len[b] .., written by fox_cache_append with the same parent and n_new)
+    over the cache.  n = 1 is a decode step.  max_len: the most tokens a sequence has, new
+    ones included (0: what the page table holds); it sets how the keys are split."""
+    B, H, n, d = q.shape
+    dev = cache.device
+    _check(q, "q", (cache.B, cache.H, n, cache.d), torch.bfloat16, dev)
+    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    if parent is not None:
+        _check(parent, "parent", (B, n), torch.int32, dev)
+    _check_lens(n_new, "n_new", B, dev)
+    if n_new is not None and (o is None or lse is None):
+        # rows that a sequence does not have are not written
+        o = torch.zeros_like(q) if o is None else o
+        lse = torch.zeros((B, H, n), device=dev) if lse is None else lse
+    if o is None:
+        o = torch.empty_like(q)
+    else:
+        _check(o, "o", (B, H, n, d), torch.bfloat16, dev)
+    if lse is None:
+        lse = torch.empty((B, H, n), device=dev, dtype=torch.float32)
+    else:
+        _check(lse, "lse", (B, H, n), torch.float32, dev)
+    lib = load()
+    if workspace is None:
+        nbytes = lib.fox_attn_cache_workspace_bytes(cache._ref, n, max_len)
+        if nbytes:
+            workspace = _workspace(nbytes, dev)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    s = default_scale(d) if scale is None else float(scale)
+    with _on_device(dev):
+        st = lib.fox_attn_cache(cache._ref, _ptr(q), _ptr(seq_len), _ptr(parent), _ptr(n_new),
+                                _ptr(o), _ptr(lse), _ptr(workspace), nbytes, n, max_len, s,
+                                _raw_stream(dev.index))
+    _raise(st, "fox_attn_cache")
+    return o, lse

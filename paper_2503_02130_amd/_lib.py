@@ -40,6 +40,8 @@ EXPORTED = (
     "fox_attn_bwd_skip_stored", "fox_attn_bwd_fixed_gate_stored_workspace_bytes",
     "fox_attn_bwd_fixed_gate_stored", "fox_attn_bwd_fixed_gate_skip_stored",
     "fox_gate_projection", "fox_gate_projection_bwd_workspace_bytes", "fox_gate_projection_bwd",
+    "fox_cache_append", "fox_cache_append_packed", "fox_cache_keep", "fox_cache_read",
+    "fox_attn_cache_workspace_bytes", "fox_attn_cache",
 )
 
 
@@ -165,6 +167,16 @@ def load() -> ctypes.CDLL:
     lib.fox_gate_projection_bwd_workspace_bytes.argtypes = [I, I, I, I, I]
     lib.fox_gate_projection_bwd.restype = I
     lib.fox_gate_projection_bwd.argtypes = [I, P, P, P, P, P, P, P, Z, I, I, I, I, P]
+    for name, args in (
+            ("fox_cache_append", [P, I, P, P, P, P, P, P, I, P]),
+            ("fox_cache_append_packed", [P, I, P, P, P, P, P, I, P]),
+            ("fox_cache_keep", [P, P, P, P, I, P]),
+            ("fox_cache_read", [P, I, P, P, P, P, P, I, P]),
+            ("fox_attn_cache", [P, P, P, P, P, P, P, P, Z, I, I, F, P])):
+        getattr(lib, name).restype = I
+        getattr(lib, name).argtypes = args
+    lib.fox_attn_cache_workspace_bytes.restype = Z
+    lib.fox_attn_cache_workspace_bytes.argtypes = [P, I, I]
     _lib = lib
     return lib
 
@@ -186,6 +198,26 @@ def _stream(t: torch.Tensor):
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+class _NoGuard:
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return False
+
+
+_NO_GUARD = _NoGuard()
+
+
+def _on_device(device):
+    """A context in which `device` is the current one (a kernel is launched on a stream of the
+    current device); nothing where it is already."""
+    return _NO_GUARD if device.index == _get_device() else torch.cuda.device(device)
 
 
 def _check(t: torch.Tensor, name: str, shape, dtype, device):

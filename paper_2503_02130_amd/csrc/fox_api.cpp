@@ -62,6 +62,39 @@ bool all_set(std::initializer_list<const void*> ps) {
   return true;
 }
 
+// The cache descriptor: its sizes, then its pointers.
+fox_status_t check_cache(const fox_cache_t* c) {
+  if (!c) return FOX_ERR_NULL;
+  if (c->n_pages <= 0 || c->max_pages <= 0 || c->B <= 0 || c->H <= 0 || c->H_kv <= 0)
+    return FOX_ERR_SHAPE;
+  if (c->H % c->H_kv != 0) return FOX_ERR_SHAPE;
+  if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1)) != 0) return FOX_ERR_SHAPE;
+  if ((long long)c->max_pages * c->page > (1LL << 30)) return FOX_ERR_SHAPE;
+  if ((long long)c->B * c->H > (1LL << 22)) return FOX_ERR_SHAPE;
+  if ((long long)c->n_pages * c->H * c->page > kMaxElems / 128) return FOX_ERR_SHAPE;
+  if (c->format != FOX_CACHE_BF16 && c->format != FOX_CACHE_E4M3) return FOX_ERR_UNSUPPORTED;
+  if (c->d != 64 && c->d != 128) return FOX_ERR_UNSUPPORTED;
+  if (!all_set({c->k, c->v, c->c, c->page_table})) return FOX_ERR_NULL;
+  if (c->format == FOX_CACHE_E4M3 && !all_set({c->k_exp, c->v_exp})) return FOX_ERR_NULL;
+  if (!all_aligned16({c->k, c->v, c->c, c->page_table, c->k_exp, c->v_exp})) return FOX_ERR_ALIGN;
+  return FOX_OK;
+}
+
+fox::CacheSpec cache_spec(const fox_cache_t* c) {
+  return fox::CacheSpec{c->format == FOX_CACHE_E4M3, c->k, c->v, c->k_exp, c->v_exp, c->c,
+                        c->page_table, c->n_pages, c->page, c->max_pages, c->B, c->H, c->H_kv,
+                        c->d};
+}
+
+bool cache_dtype(int dtype) { return dtype == FOX_DTYPE_F32 || dtype == FOX_DTYPE_BF16; }
+
+constexpr int kMaxNewTokens = 64;
+
+int cache_max_len(const fox_cache_t* c, int max_len) {
+  const int cap = c->max_pages * c->page;
+  return max_len <= 0 || max_len > cap ? cap : max_len;
+}
+
 }  // namespace
 
 extern "C" {
@@ -812,6 +845,75 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
   return launch_status(fox::launch_gate_proj_bwd(dtype == FOX_DTYPE_BF16, x, w_f, d_logit, dx,
                                                  dw_f, db_f, workspace, B, L, H, M,
                                                  static_cast<hipStream_t>(stream)));
+}
+
+fox_status_t fox_cache_append(const fox_cache_t* cache, fox_dtype_t dtype, const void* k, const void* v,
+                     const float* gate_logit, const int* seq_len, const int* parent,
+                     const int* n_new, int n, hipStream_t stream) {
+  fox_status_t st = check_cache(cache);
+  if (st) return st;
+  if (!all_set({k, v, gate_logit, seq_len})) return FOX_ERR_NULL;
+  if (n < 1 || n > kMaxNewTokens) return FOX_ERR_SHAPE;
+  if (!cache_dtype(dtype)) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({k, v, gate_logit, seq_len, parent, n_new})) return FOX_ERR_ALIGN;
+  return launch_status(fox::launch_cache_append(cache_spec(cache), dtype == FOX_DTYPE_BF16, k, v,
+                                                gate_logit, seq_len, parent, n_new, n, stream));
+}
+
+fox_status_t fox_cache_append_packed(const fox_cache_t* cache, fox_dtype_t dtype, const void* k,
+                            const void* v, const float* c, const int* cu_seqlens,
+                            const int* seq_len, int N, hipStream_t stream) {
+  fox_status_t st = check_cache(cache);
+  if (st) return st;
+  if (!all_set({k, v, c, cu_seqlens})) return FOX_ERR_NULL;
+  if (N < 1 || (long long)N * cache->H > (1LL << 31) - 1) return FOX_ERR_SHAPE;
+  if (!cache_dtype(dtype)) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({k, v, c, cu_seqlens, seq_len})) return FOX_ERR_ALIGN;
+  return launch_status(fox::launch_cache_append_packed(cache_spec(cache), dtype == FOX_DTYPE_BF16,
+                                                       k, v, c, cu_seqlens, seq_len, N, stream));
+}
+
+fox_status_t fox_cache_keep(const fox_cache_t* cache, const int* seq_len, const int* index,
+                   const int* n_keep, int n, hipStream_t stream) {
+  fox_status_t st = check_cache(cache);
+  if (st) return st;
+  if (!all_set({seq_len, index, n_keep})) return FOX_ERR_NULL;
+  if (n < 1 || n > kMaxNewTokens) return FOX_ERR_SHAPE;
+  if (!all_aligned16({seq_len, index, n_keep})) return FOX_ERR_ALIGN;
+  return launch_status(fox::launch_cache_keep(cache_spec(cache), seq_len, index, n_keep, n, stream));
+}
+
+fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const int* start,
+                   const int* seq_len, void* k, void* v, float* c, int T, hipStream_t stream) {
+  fox_status_t st = check_cache(cache);
+  if (st) return st;
+  if (!all_set({seq_len, k, v})) return FOX_ERR_NULL;
+  if (T < 1 || (long long)T * cache->B * cache->H > (1LL << 31) - 1) return FOX_ERR_SHAPE;
+  if (!cache_dtype(dtype)) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({start, seq_len, k, v, c})) return FOX_ERR_ALIGN;
+  return launch_status(fox::launch_cache_read(cache_spec(cache), dtype == FOX_DTYPE_BF16, start,
+                                              seq_len, k, v, c, T, stream));
+}
+
+size_t fox_attn_cache_workspace_bytes(const fox_cache_t* cache, int n, int max_len) {
+  if (check_cache(cache) || n < 1 || n > kMaxNewTokens) return 0;
+  return fox::attn_cache_workspace_bytes(cache_spec(cache), n, cache_max_len(cache, max_len));
+}
+
+fox_status_t fox_attn_cache(const fox_cache_t* cache, const void* q, const int* seq_len,
+                   const int* parent, const int* n_new, void* o, float* lse, void* workspace,
+                   size_t workspace_bytes, int n, int max_len, float scale, hipStream_t stream) {
+  fox_status_t st = check_cache(cache);
+  if (st) return st;
+  if (!all_set({q, seq_len, o, lse})) return FOX_ERR_NULL;
+  if (n < 1 || n > kMaxNewTokens) return FOX_ERR_SHAPE;
+  if (!all_aligned16({q, seq_len, parent, n_new, o, lse, workspace})) return FOX_ERR_ALIGN;
+  const fox::CacheSpec s = cache_spec(cache);
+  const int len = cache_max_len(cache, max_len);
+  const size_t need = fox::attn_cache_workspace_bytes(s, n, len);
+  if (need && (!workspace || workspace_bytes < need)) return FOX_ERR_WORKSPACE;
+  return launch_status(fox::launch_attn_cache(s, q, seq_len, parent, n_new, o, lse, workspace, n,
+                                              len, scale, stream));
 }
 
 }  // extern "C"

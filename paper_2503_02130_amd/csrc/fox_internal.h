@@ -186,4 +186,29 @@ hipError_t launch_gate_proj_bwd(bool bf16, const void* x, const float* w, const 
                                 void* dx, float* dw, float* db, void* ws, int B, int L, int H,
                                 int M, hipStream_t s);
 
+// The paged key/value cache (kv_cache.hip) and the attention of new tokens over it
+// (attn_cache.hip).  page is a power of two from 16 to 256.
+struct CacheSpec {
+  bool f8;
+  void *k, *v;
+  unsigned char *k_exp, *v_exp;
+  float* c;
+  const int* page_table;
+  int n_pages, page, max_pages, B, H, Hkv, d;
+};
+hipError_t launch_cache_append(const CacheSpec& s, bool bf16, const void* k, const void* v,
+                               const float* logit, const int* seq_len, const int* parent,
+                               const int* n_new, int n, hipStream_t st);
+hipError_t launch_cache_append_packed(const CacheSpec& s, bool bf16, const void* k, const void* v,
+                                      const float* c, const int* cu, const int* seq_len, int N,
+                                      hipStream_t st);
+hipError_t launch_cache_keep(const CacheSpec& s, const int* seq_len, const int* index,
+                             const int* n_keep, int n, hipStream_t st);
+hipError_t launch_cache_read(const CacheSpec& s, bool bf16, const int* start, const int* seq_len,
+                             void* k, void* v, float* c, int T, hipStream_t st);
+size_t attn_cache_workspace_bytes(const CacheSpec& s, int n, int max_len);
+hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_len,
+                             const int* parent, const int* n_new, void* o, float* lse, void* ws,
+                             int n, int max_len, float scale, hipStream_t st);
+
 }  // namespace fox

@@ -1,0 +1,375 @@
+"""The paged key/value cache: writing (quantised), moving and reading, bit for bit, and the
+attention over it, against plain 64-bit references.  Every slot that holds no token is NaN."""
+import pytest
+import torch
+
+import paper_2503_02130_amd as fox
+from cache_reference import DEV, F8, Cache, ancestors, attend, ints, log_f, quantise
+
+pytestmark = pytest.mark.gpu
+
+
+def _random_tree(n, g):
+    return [max(-1, i - 1 - int(torch.randint(0, 3, (1,), generator=g))) for i in range(n)]
+
+
+def _new_rows(cache, n, dtype, seed, scale=1.0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    shape = (cache.B, cache.Hkv, n, cache.d)
+    k, v = (scale * torch.randn(shape, generator=g, device=DEV) for _ in range(2))
+    logit = 2.0 + 2.0 * torch.randn((cache.B, cache.H, n), generator=g, device=DEV)
+    return k.to(dtype), v.to(dtype), logit
+
+
+def _expect(cache, x):
+    """What the cache stands for after rows x are written (64 bits)."""
+    return quantise(x)[0] if cache.f8 else x.to(torch.bfloat16).double()
+
+
+APPEND = [
+    # fmt, dtype, H, Hkv, d, page, n, lens, tree
+    ("e4m3", torch.bfloat16, 4, 2, 128, 16, 1, [0, 5, 15, 16], False),
+    ("e4m3", torch.float32, 6, 3, 64, 32, 7, [31, 0, 1, 90], True),
+    ("e4m3", torch.bfloat16, 8, 1, 64, 16, 64, [3, 64, 17, 0], True),
+    ("bf16", torch.bfloat16, 3, 3, 128, 64, 33, [63, 1, 0, 128], False),
+    ("bf16", torch.float32, 2, 1, 64, 256, 2, [255, 256, 254, 0], True),
+]
+
+
+@pytest.mark.parametrize("fmt,dtype,H,Hkv,d,page,n,lens,tree", APPEND)
+@pytest.mark.parametrize("ragged", [False, True])
+def test_append_and_read(fmt, dtype, H, Hkv, d, page, n, lens, tree, ragged):
+    max_pages = (max(lens) + n + page - 1) // page
+    cache = Cache(4, H, Hkv, d, page, max_pages, fmt, 11 + n)
+    cache.fill(lens)
+    before = cache.snapshot()
+    k, v, logit = _new_rows(cache, n, dtype, 12)
+    g = torch.Generator()
+    g.manual_seed(n)
+    parents = [_random_tree(n, g) for _ in lens]
+    n_new = [n, max(0, n - 3), 0, 1] if ragged else [n] * 4
+    fox.fox_cache_append(cache.dev, k, v, logit, ints(lens), ints(parents) if tree else None,
+                         ints(n_new) if ragged else None)
+    end = [x + m for x, m in zip(lens, n_new)]
+    T = max(end)
+    rk, rv, rc = fox.fox_cache_read(cache.dev, ints(end), T, dtype=torch.float32)
+    ek, ev, lf = _expect(cache, k), _expect(cache, v), log_f(logit)
+    for b in range(4):
+        L, m = lens[b], n_new[b]
+        assert torch.equal(rk[b, :, :L].double(), cache.k[b])
+        assert torch.equal(rv[b, :, :L].double(), cache.v[b])
+        assert torch.equal(rk[b, :, L:L + m].double(), ek[b, :, :m])
+        assert torch.equal(rv[b, :, L:L + m].double(), ev[b, :, :m])
+        assert not rk[b, :, L + m:].any() and not rc[b, :, L + m:].any()
+        path = ancestors(parents[b] if tree else None, m)
+        c0 = cache.c[b][:, -1] if L else torch.zeros(H, device=DEV, dtype=torch.float64)
+        for i in range(m):
+            c = c0 + lf[b][:, path[i]].sum(-1)
+            # log sigmoid in fp32 (a few 2^-24 of each term), the sum rounded once
+            tol = 2.0 ** -24 * (8 * lf[b][:, path[i]].abs().sum(-1) + 2 * c.abs())
+            assert ((rc[b, :, L + i].double() - c).abs() <= tol).all()
+    # nothing else was written
+    for x, name in zip(before, ("k", "v", "c", "k_exp", "v_exp")):
+        now = getattr(cache.dev, name).view(torch.uint8).clone()
+        for b in range(4):
+            for t in range(lens[b], end[b]):
+                p, s = cache.at(b, t)
+                e = 4 if name == "c" else 1
+                if name.endswith("exp"):
+                    now[p, :, s], x[p, :, s] = 0, 0
+                elif name == "c":
+                    now[p, :, s * e:(s + 1) * e], x[p, :, s * e:(s + 1) * e] = 0, 0
+                else:
+                    now[p, :, s], x[p, :, s] = 0, 0
+        assert torch.equal(now, x), name
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_quantised_values_of_every_size(d):
+    """Rows from the subnormal to the largest bf16, zeros, exact powers, 448 * 2^e and just
+    above; the read value is the nearest code times the scale."""
+    cache = Cache(1, 1, 1, d, 256, 1, "e4m3", 3)
+    n = 64
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    e = torch.linspace(-133, 126, n, device=DEV).round()
+    x = (torch.randn((1, 1, n, d), generator=g, device=DEV).double() *
+         torch.exp2(e.double())[:, None]).clamp(-3e38, 3e38).float().to(torch.bfloat16)
+    x[0, 0, 0] = 0
+    x[0, 0, 1, 0] = 448.0
+    x[0, 0, 2, 0] = 450.0   # bf16 above 448
+    x[0, 0, 3] = 2.0 ** 20
+    x[0, 0, 4, ::2] = 0
+    y = x.flip(2).contiguous()
+    fox.fox_cache_append(cache.dev, x, y, torch.zeros((1, 1, n), device=DEV), ints([0]))
+    k, v, _ = fox.fox_cache_read(cache.dev, ints([n]), n, dtype=torch.float32)
+    assert torch.equal(k.double(), quantise(x)[0])
+    assert torch.equal(v.double(), quantise(y)[0])
+    kb = fox.fox_cache_read(cache.dev, ints([n]), n)[0]
+    assert torch.equal(kb.double(), k.double())  # exact in bf16
+
+
+def test_values_that_are_not_finite():
+    cache = Cache(1, 1, 1, 64, 16, 1, "e4m3", 3)
+    x = torch.randn((1, 1, 3, 64), device=DEV).to(torch.bfloat16)
+    y = x.clone()
+    y[0, 0, 0, 5], y[0, 0, 1, 9], y[0, 0, 1, 10] = float("nan"), float("inf"), -float("inf")
+    fox.fox_cache_append(cache.dev, y, x, torch.zeros((1, 1, 3), device=DEV), ints([0]))
+    k = fox.fox_cache_read(cache.dev, ints([3]), 3, dtype=torch.float32)[0]
+    bad = ~torch.isfinite(y.float())
+    assert torch.equal(torch.isnan(k), bad)
+    z = torch.where(bad, 0.0, y.float())
+    assert torch.equal(torch.where(bad, 0.0, k.double()), quantise(z)[0])
+
+
+@pytest.mark.parametrize("fmt,H,Hkv,d,page,prompts,lens,dtype", [
+    ("e4m3", 4, 2, 128, 16, [1, 37, 0, 130], None, torch.bfloat16),
+    ("e4m3", 3, 1, 64, 64, [64, 65, 63, 1], [0, 7, 100, 63], torch.float32),
+    ("bf16", 2, 2, 128, 32, [300, 5, 1, 2], [1, 0, 31, 32], torch.bfloat16),
+])
+def test_append_packed(fmt, H, Hkv, d, page, prompts, lens, dtype):
+    old = lens or [0] * 4
+    max_pages = (max(a + b for a, b in zip(old, prompts)) + page - 1) // page
+    cache = Cache(4, H, Hkv, d, page, max_pages, fmt, 21)
+    cache.fill(old)
+    cu = [0]
+    for x in prompts:
+        cu.append(cu[-1] + x)
+    N = cu[-1] + 5  # rows behind the last sequence
+    g = torch.Generator(device=DEV)
+    g.manual_seed(22)
+    k, v = (torch.randn((Hkv, N, d), generator=g, device=DEV).to(dtype) for _ in range(2))
+    c = -torch.rand((H, N), generator=g, device=DEV).cumsum(-1)
+    fox.fox_cache_append_packed(cache.dev, k, v, c, ints(cu), None if lens is None else ints(lens))
+    end = [a + b for a, b in zip(old, prompts)]
+    rk, rv, rc = fox.fox_cache_read(cache.dev, ints(end), max(end) + 3, dtype=torch.float32)
+    ek, ev = _expect(cache, k), _expect(cache, v)
+    for b in range(4):
+        L, m = old[b], prompts[b]
+        rows = slice(cu[b], cu[b + 1])
+        assert torch.equal(rk[b, :, :L].double(), cache.k[b])
+        assert torch.equal(rk[b, :, L:L + m].double(), ek[:, rows])
+        assert torch.equal(rv[b, :, L:L + m].double(), ev[:, rows])
+        assert not rk[b, :, L + m:].any()
+        c0 = cache.c[b][:, -1:].float() if L else torch.zeros((H, 1), device=DEV)
+        assert torch.equal(rc[b, :, L:L + m], c0 + c[:, rows])
+
+
+@pytest.mark.parametrize("fmt,d,page", [("e4m3", 64, 16), ("e4m3", 128, 64), ("bf16", 64, 32),
+                                        ("bf16", 128, 16)])
+def test_keep(fmt, d, page):
+    """Overlapping moves, the same index twice, out of order, none and all."""
+    n, lens = 64, [0, 3, 50, 16, 7]
+    index = [list(range(n)), [0, 2, 3, 7, 20, 40, 63], [5, 5, 1, 0, 0], [], [63] * 64]
+    cache = Cache(5, 4, 2, d, page, (50 + n + page - 1) // page, fmt, 31)
+    cache.fill([x + n for x in lens])
+    rows = [x + [-1] * (n - len(x)) for x in index]
+    fox.fox_cache_keep(cache.dev, ints(lens), ints(rows), ints([len(x) for x in index]))
+    end = [x + n for x in lens]
+    k, v, c = fox.fox_cache_read(cache.dev, ints(end), max(end), dtype=torch.float32)
+    for b, L in enumerate(lens):
+        at = list(range(end[b]))
+        at[L:L + len(index[b])] = [L + i for i in index[b]]
+        assert torch.equal(k[b, :, :end[b]].double(), cache.k[b][:, at])
+        assert torch.equal(v[b, :, :end[b]].double(), cache.v[b][:, at])
+        assert torch.equal(c[b, :, :end[b]].double(), cache.c[b][:, at])
+
+
+def _attn_check(cache, lens, n_new, parents, q, o, lse, scale, missing=()):
+    """missing: (b, table index) of pages that do not exist."""
+    n = q.shape[2]
+    for b, L in enumerate(lens):
+        m = n_new[b]
+        gone = {t for bb, p in missing if bb == b
+                for t in range(p * cache.page, (p + 1) * cache.page)}
+        seen = []
+        for i, path in enumerate(ancestors(None if parents is None else parents[b], m)):
+            at = list(range(L)) + sorted(L + j for j in path)
+            seen.append([] if L + i in gone else [t for t in at if t not in gone])
+        ro, rl, to, tl = attend(q[b][:, :m], cache.k[b], cache.v[b], cache.c[b], L, seen, scale)
+        err = (o[b][:, :m].double() - ro).abs()
+        assert (err <= to).all(), f"sequence {b}: {float((err / to).max()):.2f} of the bound"
+        empty = torch.isinf(rl)
+        assert torch.equal(torch.isinf(lse[b][:, :m]), empty)
+        el = torch.where(empty, 0.0, (lse[b][:, :m].double() - rl).abs())
+        assert (el <= tl).all(), f"sequence {b}: lse {float((el / tl).max()):.2f} of the bound"
+
+
+ATTN = [
+    # fmt, H, Hkv, d, page, n, lens, tree
+    ("bf16", 1, 1, 64, 16, 1, [0, 1, 15, 16], False),       # a first token, ends of pages
+    ("e4m3", 1, 1, 64, 16, 1, [0, 1, 31, 200], False),
+    ("e4m3", 4, 1, 128, 64, 1, [63, 64, 127, 500], False),  # decode, four heads to a key head
+    ("bf16", 16, 2, 128, 32, 1, [33, 700, 129, 0], False),
+    ("e4m3", 12, 4, 64, 16, 5, [0, 40, 77, 128], True),
+    ("bf16", 6, 2, 64, 256, 8, [250, 256, 300, 2], True),   # 24 rows: two row tiles
+    ("e4m3", 4, 2, 128, 16, 16, [100, 3, 0, 257], False),   # a chain, 32 rows
+    ("bf16", 4, 2, 128, 64, 23, [10, 64, 333, 100], True),  # 46 rows, ragged row tile
+    ("e4m3", 4, 4, 128, 128, 64, [60, 128, 1000, 7], True),
+    ("bf16", 10, 2, 64, 16, 33, [5, 0, 90, 400], True),     # 165 rows: row blocks
+    ("e4m3", 32, 1, 64, 32, 1, [100, 5, 31, 600], False),   # 32 heads to a key head
+]
+
+
+@pytest.mark.parametrize("fmt,H,Hkv,d,page,n,lens,tree", ATTN)
+@pytest.mark.parametrize("ragged", [False, True])
+def test_attention(fmt, H, Hkv, d, page, n, lens, tree, ragged):
+    print(fmt, H, Hkv, d, page, n, lens, tree, ragged, flush=True)
+    max_pages = (max(lens) + n + page - 1) // page + 1
+    cache = Cache(4, H, Hkv, d, page, max_pages, fmt, 41 + n)
+    n_new = [n, max(0, n - 1), max(1, n // 2), n] if ragged else [n] * 4
+    cache.fill([a + b for a, b in zip(lens, n_new)])
+    g = torch.Generator()
+    g.manual_seed(n)
+    parents = [_random_tree(n, g) for _ in lens] if tree else None
+    q = torch.randn((4, H, n, d), device=DEV, generator=cache.g).to(torch.bfloat16)
+    o = torch.full_like(q, 7.0)
+    lse = torch.full((4, H, n), 7.0, device=DEV)
+    scale = fox.default_scale(d)
+    fox.fox_attn_cache(q, cache.dev, ints(lens), ints(parents) if tree else None,
+                       ints(n_new) if ragged else None, o=o, lse=lse)
+    _attn_check(cache, lens, n_new, parents, q, o, lse, scale)
+    for b in range(4):  # rows that a sequence does not have
+        assert (o[b][:, n_new[b]:] == 7).all() and (lse[b][:, n_new[b]:] == 7).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+@pytest.mark.parametrize("max_len", [0, 1, 3003, 5000])
+def test_attention_splits(fmt, max_len):
+    """One sequence over many splits, whatever max_len says of its length; a strong gate whose
+    far keys vanish, and a weak one."""
+    for mean in (-3.0, 8.0):
+        cache = Cache(1, 4, 2, 64, 16, 190, fmt, 51)
+        cache.fill([3003], mean=mean)
+        q = torch.randn((1, 4, 3, 64), device=DEV, generator=cache.g).to(torch.bfloat16)
+        o, lse = fox.fox_attn_cache(q, cache.dev, ints([3000]), max_len=max_len)
+        _attn_check(cache, [3000], [3], None, q, o, lse, fox.default_scale(64))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+def test_pages_that_do_not_exist(fmt):
+    """A context page, the page of the new tokens, and places past the table."""
+    cache = Cache(3, 2, 1, 64, 16, 4, fmt, 61)
+    lens, n = [40, 46, 62], 4
+    cache.fill([44, 50, 64])
+    cache.table[0, 1] = -1
+    cache.table[1, 3] = 1 << 30
+    before = cache.snapshot()
+    q = torch.randn((3, 2, n, 64), device=DEV, generator=cache.g).to(torch.bfloat16)
+    o, lse = fox.fox_attn_cache(q, cache.dev, ints(lens))
+    for b in range(3):  # pad the references to the asked length
+        pad = lens[b] + n - cache.k[b].shape[1]
+        if pad > 0:
+            cache.k[b] = torch.nn.functional.pad(cache.k[b], (0, 0, 0, pad))
+            cache.v[b] = torch.nn.functional.pad(cache.v[b], (0, 0, 0, pad))
+            cache.c[b] = torch.nn.functional.pad(cache.c[b], (0, pad))
+    missing = [(0, 1), (1, 3), (2, 4)]
+    _attn_check(cache, lens, [n] * 3, None, q, o, lse, fox.default_scale(64), missing)
+    # reading leaves such rows as they were, writing and moving skip them
+    k = torch.full((3, 1, 66, 64), 3.0, device=DEV)
+    v, c = torch.full_like(k, 3.0), torch.full((3, 2, 66), 3.0, device=DEV)
+    fox.fox_cache_read(cache.dev, ints([66, 66, 66]), 66, k=k, v=v, c=c)
+    assert (k[0, :, 16:32] == 3).all() and (k[1, :, 48:64] == 3).all() and (k[:, :, 64:] == 3).all()
+    assert (c[0, :, 16:32] == 3).all() and (c[:, :, 64:] == 3).all()
+    kn, vn, logit = _new_rows(cache, n, torch.bfloat16, 62)
+    fox.fox_cache_append(cache.dev, kn, vn, logit, ints([16, 60, 1 << 30]), None, ints([n, n, n]))
+    fox.fox_cache_keep(cache.dev, ints([14, 60, 64]), ints([[3, 2, 1, 0]] * 3), ints([2, 4, 4]))
+    assert all(torch.equal(a, b) for a, b in zip(before, cache.snapshot()))
+
+
+def test_one_row_alone_and_in_a_batch():
+    """What other sequences hold does not change a sequence's bits."""
+    cache = Cache(3, 4, 2, 128, 64, 8, "e4m3", 71)
+    cache.fill([400, 100, 257])
+    q = torch.randn((3, 4, 1, 128), device=DEV, generator=cache.g).to(torch.bfloat16)
+    a = fox.fox_attn_cache(q, cache.dev, ints([399, 99, 256]))
+    b = fox.fox_attn_cache(q, cache.dev, ints([0, 99, 3]))
+    assert torch.equal(a[0][1], b[0][1]) and torch.equal(a[1][1], b[1][1])
+    again = fox.fox_attn_cache(q, cache.dev, ints([399, 99, 256]))
+    assert torch.equal(a[0], again[0]) and torch.equal(a[1], again[1])
+
+
+def test_decode_agrees_with_the_contiguous_cache():
+    """H = H_kv, a bf16 cache: fox_attn_decode's result, to the roundings of both."""
+    B, H, T, d = 3, 4, 777, 128
+    cache = Cache(B, H, H, d, 64, 13, "bf16", 81)
+    cache.fill([T] * B)
+    q = torch.randn((B, H, 1, d), device=DEV, generator=cache.g).to(torch.bfloat16)
+    o, lse = fox.fox_attn_cache(q, cache.dev, ints([T - 1] * B))
+    k, v = (torch.stack(x).to(torch.bfloat16).contiguous() for x in (cache.k, cache.v))
+    c = torch.stack(cache.c).float()
+    # a logit whose log sigmoid is the last step of c
+    step = (torch.stack(cache.c)[..., -1] - torch.stack(cache.c)[..., -2])
+    logit = (step - torch.log(-torch.expm1(step))).float().contiguous()
+    o2, lse2 = fox.fox_attn_decode(q[:, :, 0].contiguous(), k, v, c.contiguous(), logit)
+    assert (o[:, :, 0].double() - o2.double()).norm() <= 4 * 2.0 ** -8 * o2.double().norm()
+    assert (lse[:, :, 0] - lse2).abs().max() <= 2.0 ** -7
+
+
+def test_step_in_a_graph():
+    """Append, attend, keep captured and replayed with new inputs and lengths, against the
+    same calls run eagerly; two captured graphs with a workspace each."""
+    B, H, Hkv, d, n, page = 2, 4, 2, 64, 8, 16
+    lens = [600, 37]
+
+    def fresh():
+        cache = Cache(B, H, Hkv, d, page, 48, "e4m3", 91)
+        cache.fill(lens)
+        return cache
+
+    cache, other = fresh(), fresh()
+    k, v, logit = _new_rows(cache, n, torch.bfloat16, 92)
+    q = torch.randn((B, H, n, d), device=DEV, generator=cache.g).to(torch.bfloat16)
+    par, idx = ints([[-1, 0, 0, 1, 2, 3, 5, 6]] * B), ints([[0, 1, 3, 5, 6, 7, 0, 0]] * B)
+    seq, keep = ints(lens), ints([6, 2])
+
+    def step(cache, seq, ws, o, lse):
+        fox.fox_cache_append(cache.dev, k, v, logit, seq, par)
+        fox.fox_attn_cache(q, cache.dev, seq, par, o=o, lse=lse, workspace=ws)
+        fox.fox_cache_keep(cache.dev, seq, idx, keep)
+        seq += keep
+
+    nbytes = max(16, fox.fox_attn_cache_workspace_bytes(cache.dev, n))
+    ws = [torch.empty(nbytes, device=DEV, dtype=torch.uint8) for _ in range(3)]
+    outs = [(torch.empty_like(q), torch.empty((B, H, n), device=DEV)) for _ in range(3)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(cache, seq, ws[0], *outs[0])
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    seq2 = seq.clone()
+    for name in ("k", "v", "c", "k_exp", "v_exp", "page_table"):
+        getattr(other.dev, name).view(torch.uint8).copy_(getattr(cache.dev, name).view(torch.uint8))
+    graphs = []
+    for i in range(2):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            step(cache, seq, ws[i], *outs[i])
+        graphs.append(gr)
+    for i in range(4):
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, device=DEV, generator=cache.g))
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        step(other, seq2, ws[2], *outs[2])
+        torch.cuda.synchronize()
+        assert torch.equal(seq, seq2)
+        assert torch.equal(outs[i % 2][0], outs[2][0]) and torch.equal(outs[i % 2][1], outs[2][1])
+        # bits, not values: unused slots are NaN
+        assert all(torch.equal(a, b) for a, b in zip(cache.snapshot(), other.snapshot()))
+
+
+def test_another_stream():
+    cache = Cache(2, 4, 2, 128, 64, 10, "e4m3", 95)
+    cache.fill([500, 333])
+    q = torch.randn((2, 4, 1, 128), device=DEV, generator=cache.g).to(torch.bfloat16)
+    want = fox.fox_attn_cache(q, cache.dev, ints([499, 332]))
+    seq = ints([499, 332])
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = fox.fox_attn_cache(q, cache.dev, seq)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
