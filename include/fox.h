@@ -517,6 +517,58 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
                             size_t workspace_bytes, int B, int L, int H, int M, hipStream_t stream);
 
 /*
+ * Packed sequences with grouped heads: B sequences of different lengths, one behind the
+ * other, without padding.  Query head h reads key head h / (H / H_kv) and has its own forget
+ * gate; H is a multiple of H_kv.
+ *
+ *   q, o, d_o, dq  [H,N,d] dtype     k, v, dk, dv  [H_kv,N,d] dtype
+ *   gate logits    [H,N] fp32 or bf16 (gate_dtype)     c, lse [H,N] fp32
+ *   cu_seqlens     [B+1] int32, on the device: sequence b is rows cu_seqlens[b] ..
+ *                  cu_seqlens[b+1] - 1; the first is 0, the last at most N, none is smaller
+ *                  than the one before (a sequence may be empty).  Rows behind the last
+ *                  sequence are neither read nor written, except by fox_packed_zero_behind.
+ *   N * H and the rows of a head in bytes must be below 2^31.
+ *
+ * fox_packed_plan: the list of 128-row blocks that the attention calls walk, the heaviest
+ *   first, into a device buffer of fox_packed_plan_bytes(); made once for a batch and used by
+ *   every layer's forward and backward.
+ * fox_gate_prefix_packed: c, the running sum of log sigmoid(gate_logit) within each sequence
+ *   (summed in 64 bits, rounded once).
+ * fox_attn_fwd_packed: O and LSE of each sequence as fox_attn_fwd's.  max_len: the longest
+ *   sequence, if known, else 0 (N): it decides how the work is split, not what is computed.
+ * fox_attn_bwd_packed: the gradients of sum(O o dO): dq, dk, dv (dk, dv summed over the query
+ *   heads of a key head) and d_logit in gate_dtype, the gradient of the gate logits; d_log_f
+ *   [H,N] fp32, that of log f, may be NULL.  workspace: at least
+ *   fox_attn_bwd_packed_workspace_bytes().
+ * fox_packed_zero_behind: writes zeros to the rows behind the last sequence of n (at most 8)
+ *   tensors [heads, N, row_bytes] on the device; row_bytes even.
+ */
+typedef struct {
+  void* x;
+  int heads;
+  int row_bytes;
+} fox_packed_rows_t;
+
+size_t fox_packed_plan_bytes(int B, int N);
+fox_status_t fox_packed_plan(const int* cu_seqlens, int B, int N, void* plan, size_t plan_bytes,
+                    hipStream_t stream);
+fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_logit,
+                           const int* cu_seqlens, float* c, int B, int H, int N,
+                           hipStream_t stream);
+fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
+                        const float* c, const void* plan, void* o, float* lse, int B, int H,
+                        int H_kv, int N, int d, int max_len, float scale, hipStream_t stream);
+size_t fox_attn_bwd_packed_workspace_bytes(int H, int N);
+fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
+                        const float* c, const void* o, const float* lse, const void* d_o,
+                        fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
+                        const void* plan, void* dq, void* dk, void* dv, void* d_logit,
+                        float* d_log_f, void* workspace, size_t workspace_bytes, int B, int H,
+                        int H_kv, int N, int d, int max_len, float scale, hipStream_t stream);
+fox_status_t fox_packed_zero_behind(const fox_packed_rows_t* tensors, int n, const int* cu_seqlens,
+                           int B, int N, hipStream_t stream);
+
+/*
  * A paged key/value cache for serving, with grouped heads: query head h reads key head
  * h / (H / H_kv) and has its own forget gate.
  *

@@ -15,6 +15,7 @@ from typing import Optional
 import torch
 
 from . import _lib as fox
+from . import _packed
 
 
 class ForgettingAttention(torch.autograd.Function):
@@ -52,6 +53,49 @@ def forgetting_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     """
     s = fox.default_scale(q.shape[-1]) if scale is None else float(scale)
     return ForgettingAttention.apply(q, k, v, gate_logit, s, keep_ds)
+
+
+class PackedForgettingAttention(torch.autograd.Function):
+    """o [H,N,d] of packed sequences: q [H,N,d], k, v [H_kv,N,d], gate logits [H,N]."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        gate_logit = gate_logit.contiguous()
+        if plan is None:
+            plan = _packed.fox_packed_plan(cu_seqlens, q.shape[1])
+        c = _packed.fox_gate_prefix_packed(gate_logit, cu_seqlens)
+        o, lse = _packed.fox_attn_fwd_packed(q, k, v, c, cu_seqlens, plan, max_len, scale)
+        _packed.fox_packed_zero_behind((o,), cu_seqlens)
+        ctx.save_for_backward(q, k, v, gate_logit, c, o, lse, cu_seqlens, plan)
+        ctx.max_len, ctx.scale = max_len, scale
+        return o
+
+    @staticmethod
+    def backward(ctx, d_o):
+        q, k, v, gate_logit, c, o, lse, cu_seqlens, plan = ctx.saved_tensors
+        d_o = d_o.to(q.dtype).contiguous()
+        grads = _packed.fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit, cu_seqlens,
+                                            plan, ctx.max_len, ctx.scale)
+        _packed.fox_packed_zero_behind(grads, cu_seqlens)
+        return (*grads, None, None, None, None)
+
+
+def forgetting_attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                                gate_logit: torch.Tensor, cu_seqlens: torch.Tensor,
+                                max_len: int = 0, scale: Optional[float] = None,
+                                plan: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal Forgetting Attention of packed sequences with grouped heads, with autograd
+    support.
+
+    q: [H, N, d], k, v: [H_kv, N, d] bf16 or fp32 on the GPU (d = 64 or 128, H a multiple of
+    H_kv); gate_logit: [H, N] fp32 or bf16; cu_seqlens: [B + 1] int32, sequence b being rows
+    cu_seqlens[b] .. cu_seqlens[b + 1] - 1.  max_len: the longest sequence, if known (it sets
+    how the work is split).  plan: fox_packed_plan(cu_seqlens, N), to share it between layers.
+    The output and the gradients are zero in rows behind the last sequence.
+    """
+    s = fox.default_scale(q.shape[-1]) if scale is None else float(scale)
+    return PackedForgettingAttention.apply(q, k, v, gate_logit, cu_seqlens, plan, max_len, s)
 
 
 class GateProjection(torch.autograd.Function):

@@ -40,10 +40,14 @@
 //   * The gate bias c_i - c_j is formed in natural-log units before the change to
 //     base 2, so the row maximum stays small and the logsumexp carries no
 //     cancellation even when c changes by thousands within a block.
+//   * Packed sequences (PK): the row blocks are the quarters of the plan's items, K and V
+//     belong to key heads of G query heads each, and dK and dV of a key block sum over the G
+//     heads in registers, one head after the other.
 #include <algorithm>
 
 #include "fox_device.h"
 #include "fox_internal.h"
+#include "packed.h"
 
 namespace fox {
 
@@ -163,6 +167,42 @@ __device__ __forceinline__ f32x4 f32_get_partial(const char* slice, int row, int
   return *reinterpret_cast<const f32x4*>(slice + row * D * 4 + ((chunk ^ (row & 15)) * 16));
 }
 
+// Where row block blk of a launch lies: the sequence's length L, its block mb of 32 rows, the
+// rows at which the sequence begins in q-like and in k-like tensors (dense: the same).
+struct F32Packed {
+  const PackedItem* plan;
+  int n_items, H, Hkv, N;
+};
+struct F32Place {
+  int bh, mb, L;
+  size_t row, kv_row;
+};
+template <bool PK>
+__device__ __forceinline__ long long f32_blocks(int n_blk, int BH, const F32Packed& pk, int heads) {
+  return PK ? 4LL * pk.n_items * heads : (long long)n_blk * BH;
+}
+// queries: longest rows first
+template <bool PK>
+__device__ __forceinline__ bool f32_query_place(long long blk, int n_blk, int BH, int L,
+                                                const F32Packed& pk, F32Place& p) {
+  if constexpr (PK) {
+    const PackedItem it = pk.plan[blk / (4 * pk.H)];
+    const int i = (int)(blk % (4 * pk.H));
+    p.bh = packed_head(i % pk.H, pk.Hkv, pk.H / pk.Hkv);
+    p.mb = 4 * it.block + 3 - i / pk.H;
+    p.L = it.len;
+    p.row = (size_t)p.bh * pk.N + it.start;
+    p.kv_row = (size_t)(p.bh / (pk.H / pk.Hkv)) * pk.N + it.start;
+    return 32 * p.mb < it.len;
+  } else {
+    p.bh = (int)(blk % BH);
+    p.mb = n_blk - 1 - (int)(blk / BH);
+    p.L = L;
+    p.row = p.kv_row = (size_t)p.bh * (size_t)L;
+    return true;
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Forward.
 // ---------------------------------------------------------------------------
@@ -173,12 +213,12 @@ struct F32FwdSmem {
   float m[NW][32], l[NW][32];
 };
 
-template <int D, bool FIXED, int NW>
+template <int D, bool FIXED, int NW, bool PK = false>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1)))
 void fwd_f32_kernel(const float* __restrict__ Q, const float* __restrict__ K,
                     const float* __restrict__ V, const float* __restrict__ gate,
-                    float* __restrict__ O, float* __restrict__ LSE, int BH, int H, int L,
-                    int n_blk, float scale_log2) {
+                    float* __restrict__ O, float* __restrict__ LSE, int BH, int H, int L_,
+                    int n_blk, float scale_log2, F32Packed pk) {
   constexpr int NL = f32_tile_loads<D>();
   constexpr int NVC = NL + (FIXED ? 0 : 1);  // loads of a V tile and its prefix values
   __shared__ F32FwdSmem<D, NW> sm;
@@ -188,18 +228,19 @@ void fwd_f32_kernel(const float* __restrict__ Q, const float* __restrict__ K,
   const uint32_t dma_off = f32_dma_offset<D>(lane);
   const F32Reads<D> kt(sm.tile[wave][0], col, h), vt(sm.tile[wave][1], col, h);
   const lds_byte* c_at = lds_opaque(lds_ptr(&sm.c[wave][4 * h]));
-  const long long n_all = (long long)n_blk * BH;
+  const long long n_all = f32_blocks<PK>(n_blk, BH, pk, pk.H);
 
   for (long long blk = blockIdx.x; blk < n_all; blk += gridDim.x) {
-    const int bh = (int)(blk % BH);
-    const int mb = n_blk - 1 - (int)(blk / BH);  // longest rows first
-    const size_t head = (size_t)bh * (size_t)L;
+    F32Place at;
+    if (!f32_query_place<PK>(blk, n_blk, BH, L_, pk, at)) continue;
+    const int bh = at.bh, mb = at.mb, L = at.L;
+    const size_t head = at.row;
     const int q0 = mb * 32;
     const int qi = q0 + col;
     const bool q_valid = qi < L;
     const GateRow<FIXED> gr(gate, bh, H, head);
-    const __amdgpu_buffer_rsrc_t rk = make_rsrc(K + head * D, (uint32_t)L * D * 4);
-    const __amdgpu_buffer_rsrc_t rv = make_rsrc(V + head * D, (uint32_t)L * D * 4);
+    const __amdgpu_buffer_rsrc_t rk = make_rsrc(K + at.kv_row * D, (uint32_t)L * D * 4);
+    const __amdgpu_buffer_rsrc_t rv = make_rsrc(V + at.kv_row * D, (uint32_t)L * D * 4);
     const __amdgpu_buffer_rsrc_t rc = make_rsrc(FIXED ? K : gate + head, (uint32_t)L * 4);
 
     f32x4 qf[D / 8];
@@ -307,14 +348,14 @@ struct F32DqSmem {
   float dc[NW][32];
 };
 
-template <int D, bool FIXED, int NW>
+template <int D, bool FIXED, int NW, bool PK = false>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1)))
 void bwd_dq_f32_kernel(const float* __restrict__ Q, const float* __restrict__ K,
                        const float* __restrict__ V, const float* __restrict__ gate,
                        const float* __restrict__ LSE, const float* __restrict__ dO,
                        const float* __restrict__ delta, float* __restrict__ dQ,
-                       float* __restrict__ dcq, int BH, int H, int L, int n_blk, float scale,
-                       float scale_log2) {
+                       float* __restrict__ dcq, int BH, int H, int L_, int n_blk, float scale,
+                       float scale_log2, F32Packed pk) {
   constexpr int NL = f32_tile_loads<D>();
   __shared__ F32DqSmem<D, NW> sm;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -323,18 +364,19 @@ void bwd_dq_f32_kernel(const float* __restrict__ Q, const float* __restrict__ K,
   const uint32_t dma_off = f32_dma_offset<D>(lane);
   const F32Reads<D> kt(sm.tile[wave][0], col, h), vt(sm.tile[wave][1], col, h);
   const lds_byte* c_at = lds_opaque(lds_ptr(&sm.c[wave][4 * h]));
-  const long long n_all = (long long)n_blk * BH;
+  const long long n_all = f32_blocks<PK>(n_blk, BH, pk, pk.H);
 
   for (long long blk = blockIdx.x; blk < n_all; blk += gridDim.x) {
-    const int bh = (int)(blk % BH);
-    const int mb = n_blk - 1 - (int)(blk / BH);
-    const size_t head = (size_t)bh * (size_t)L;
+    F32Place at;
+    if (!f32_query_place<PK>(blk, n_blk, BH, L_, pk, at)) continue;
+    const int bh = at.bh, mb = at.mb, L = at.L;
+    const size_t head = at.row;
     const int q0 = mb * 32;
     const int qi = q0 + col;
     const bool q_valid = qi < L;
     const GateRow<FIXED> gr(gate, bh, H, head);
-    const __amdgpu_buffer_rsrc_t rk = make_rsrc(K + head * D, (uint32_t)L * D * 4);
-    const __amdgpu_buffer_rsrc_t rv = make_rsrc(V + head * D, (uint32_t)L * D * 4);
+    const __amdgpu_buffer_rsrc_t rk = make_rsrc(K + at.kv_row * D, (uint32_t)L * D * 4);
+    const __amdgpu_buffer_rsrc_t rv = make_rsrc(V + at.kv_row * D, (uint32_t)L * D * 4);
     const __amdgpu_buffer_rsrc_t rc = make_rsrc(FIXED ? K : gate + head, (uint32_t)L * 4);
 
     f32x4 qf[D / 8], gf[D / 8];
@@ -427,14 +469,14 @@ struct F32KvSmem {
   float dc[NW][32];
 };
 
-template <int D, bool FIXED, int NW>
+template <int D, bool FIXED, int NW, bool PK = false>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1)))
 void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ K,
                          const float* __restrict__ V, const float* __restrict__ gate,
                          const float* __restrict__ LSE, const float* __restrict__ dO,
                          const float* __restrict__ delta, float* __restrict__ dK,
-                         float* __restrict__ dV, float* __restrict__ dck, int BH, int H, int L,
-                         int n_blk, float scale, float scale_log2) {
+                         float* __restrict__ dV, float* __restrict__ dck, int BH, int H, int L_,
+                         int n_blk, float scale, float scale_log2, F32Packed pk) {
   constexpr int NL = f32_tile_loads<D>();
   __shared__ F32KvSmem<D, NW> sm;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -443,33 +485,47 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
   const uint32_t dma_off = f32_dma_offset<D>(lane);
   const F32Reads<D> qt(sm.tile[wave][0], col, h), gt(sm.tile[wave][1], col, h);
   const lds_byte* row_at = lds_opaque(lds_ptr(&sm.row[wave][0][4 * h]));
-  const long long n_all = (long long)n_blk * BH;
+  const int G = PK ? pk.H / pk.Hkv : 1;
+  const long long n_all = f32_blocks<PK>(n_blk, BH, pk, pk.Hkv);
 
   for (long long blk = blockIdx.x; blk < n_all; blk += gridDim.x) {
-    const int bh = (int)(blk % BH);
-    const int kb = (int)(blk / BH);  // key block 0 has the most work: first
-    const size_t head = (size_t)bh * (size_t)L;
+    int bh = (int)(blk % BH), L = L_;
+    int kb = (int)(blk / BH);  // key block 0 has the most work: first
+    size_t head = (size_t)bh * (size_t)L, kv_row = head;
+    if constexpr (PK) {
+      // an item's block m, as keys, is block n - 1 - m of the sequence's n
+      const PackedItem it = pk.plan[blk / (4 * pk.Hkv)];
+      const int i = (int)(blk % (4 * pk.Hkv)), hk = i % pk.Hkv;
+      L = it.len;
+      kb = 4 * ((L + kPackedBlock - 1) / kPackedBlock - 1 - it.block) + i / pk.Hkv;
+      if (L <= 0 || 32 * kb >= L) continue;
+      bh = hk * G;
+      head = (size_t)bh * pk.N + it.start;
+      kv_row = (size_t)hk * pk.N + it.start;
+    }
     const int k0 = kb * 32;
     const int kj = k0 + col;
     const bool k_valid = kj < L;
+
+    f32x4 kf[D / 8], vf[D / 8];
+    f32_load_row<D>(K + (kv_row + kj) * D, k_valid, h, kf);
+    f32_load_row<D>(V + (kv_row + kj) * D, k_valid, h, vf);
+    f32x16 ak[D / 32], av[D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) ak[db] = av[db] = f32x16{};
+    const int n_tiles = (L + 31) / 32;
+
+    // the query heads of this key head (dense: one)
+    for (int g = 0; g < G; ++g, head += PK ? pk.N : 0) {
     const GateRow<FIXED> gr(gate, bh, H, head);
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(Q + head * D, (uint32_t)L * D * 4);
     const __amdgpu_buffer_rsrc_t rg = make_rsrc(dO + head * D, (uint32_t)L * D * 4);
     const __amdgpu_buffer_rsrc_t rc = make_rsrc(FIXED ? Q : gate + head, (uint32_t)L * 4);
     const __amdgpu_buffer_rsrc_t rl = make_rsrc(LSE + head, (uint32_t)L * 4);
     const __amdgpu_buffer_rsrc_t rd = make_rsrc(delta + head, (uint32_t)L * 4);
-
-    f32x4 kf[D / 8], vf[D / 8];
-    f32_load_row<D>(K + (head + kj) * D, k_valid, h, kf);
-    f32_load_row<D>(V + (head + kj) * D, k_valid, h, vf);
     const float c_k0 = gr.raw(k0);
     const float ck = k_valid ? gr.diff(kj, k0) : 0.0f;
-    f32x16 ak[D / 32], av[D / 32];
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) ak[db] = av[db] = f32x16{};
     float dc = 0.0f;
-
-    const int n_tiles = (L + 31) / 32;
     auto issue_q = [&](int j) {
       f32_dma_tile<D>(rq, sm.tile[wave][0], dma_off, 32 * j);
       const uint32_t off = (uint32_t)(32 * j + lane) * 4;
@@ -513,11 +569,22 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
       sched_fence();  // every read of the dO tile is done
       if (more) issue_g(j + NW);
     }
+    const float dct = wave_sum_pair(dc);
+    if (h == 0) sm.dc[wave][col] = dct;
+    if constexpr (PK) {  // dc^k belongs to a query head
+      __syncthreads();
+      if (tid < 32 && k0 + tid < L) {
+        float dt = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) dt += sm.dc[w][tid];
+        dck[head + k0 + tid] = dt;
+      }
+      __syncthreads();  // the next head writes the sums again
+    }
+    }  // query heads
 
     f32_put_partial<D>(sm.tile[wave][0], ak, col, h);
     f32_put_partial<D>(sm.tile[wave][1], av, col, h);
-    const float dct = wave_sum_pair(dc);
-    if (h == 0) sm.dc[wave][col] = dct;
     __syncthreads();
     for (int item = tid; item < 32 * (D / 4); item += 64 * NW) {
       const int kr = item / (D / 4), chunk = item % (D / 4);
@@ -530,9 +597,9 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
         dt += sm.dc[w][kr];
       }
       if (k0 + kr < L) {
-        *reinterpret_cast<f32x4*>(dK + (head + k0 + kr) * D + 4 * chunk) = ok * scale;
-        *reinterpret_cast<f32x4*>(dV + (head + k0 + kr) * D + 4 * chunk) = ov;
-        if (chunk == 0) dck[head + k0 + kr] = dt;
+        *reinterpret_cast<f32x4*>(dK + (kv_row + k0 + kr) * D + 4 * chunk) = ok * scale;
+        *reinterpret_cast<f32x4*>(dV + (kv_row + k0 + kr) * D + 4 * chunk) = ov;
+        if (!PK && chunk == 0) dck[head + k0 + kr] = dt;
       }
     }
     if (n_all > gridDim.x) __syncthreads();
@@ -572,7 +639,7 @@ static void fwd_f32_t(const float* q, const float* k, const float* v, GateSpec g
     if (!f32_fine<D>(n, BH))
       return fwd_f32_t<D, FIXED, NW / 2>(q, k, v, g, o, lse, BH, L, sl2, s);
   hipLaunchKernelGGL((fwd_f32_kernel<D, FIXED, NW>), f32_grid(n, BH), dim3(64 * NW), 0, s, q, k, v,
-                     g.ptr, o, lse, BH, g.H, L, n, sl2);
+                     g.ptr, o, lse, BH, g.H, L, n, sl2, F32Packed{});
 }
 
 hipError_t launch_fwd_f32(const float* q, const float* k, const float* v, GateSpec g, float* o,
@@ -599,7 +666,7 @@ static void dkdv_f32_t(const float* q, const float* k, const float* v, GateSpec 
                                           s);
   hipLaunchKernelGGL((bwd_dkdv_f32_kernel<D, FIXED, NW>), f32_grid(n, BH), dim3(64 * NW), 0, s, q,
                      k, v, g.ptr, lse, d_o, delta, dk, dv, dck, BH, g.H, L, n, scale,
-                     scale * kLog2e);
+                     scale * kLog2e, F32Packed{});
 }
 
 hipError_t launch_bwd_dkdv_f32(const float* q, const float* k, const float* v, GateSpec g,
@@ -625,7 +692,8 @@ static void dq_f32_t(const float* q, const float* k, const float* v, GateSpec g,
     if (!f32_fine<D>(n, BH))
       return dq_f32_t<D, FIXED, NW / 2>(q, k, v, g, lse, d_o, delta, dq, dcq, BH, L, scale, s);
   hipLaunchKernelGGL((bwd_dq_f32_kernel<D, FIXED, NW>), f32_grid(n, BH), dim3(64 * NW), 0, s, q, k,
-                     v, g.ptr, lse, d_o, delta, dq, dcq, BH, g.H, L, n, scale, scale * kLog2e);
+                     v, g.ptr, lse, d_o, delta, dq, dcq, BH, g.H, L, n, scale, scale * kLog2e,
+                     F32Packed{});
 }
 
 hipError_t launch_bwd_dq_f32(const float* q, const float* k, const float* v, GateSpec g,
@@ -638,6 +706,65 @@ hipError_t launch_bwd_dq_f32(const float* q, const float* k, const float* v, Gat
     if (g.fixed) dq_f32_t<64, true, 8>(q, k, v, g, lse, d_o, delta, dq, dcq, BH, L, scale, s);
     else dq_f32_t<64, false, 8>(q, k, v, g, lse, d_o, delta, dq, dcq, BH, L, scale, s);
   }
+  return hipGetLastError();
+}
+
+// Packed sequences.  The lengths are on the device: the waves' split goes by the most row
+// blocks that the rows can make.
+template <int D, int NW>
+static void packed_fwd_f32_t(const float* q, const float* k, const float* v, const float* c,
+                             float* o, float* lse, const F32Packed& pk, float sl2, hipStream_t s) {
+  const long long blocks = 4LL * pk.n_items * pk.H;
+  if constexpr (NW == kF32Nw<D>)
+    if (blocks > kF32FineGroups)
+      return packed_fwd_f32_t<D, NW / 2>(q, k, v, c, o, lse, pk, sl2, s);
+  hipLaunchKernelGGL((fwd_f32_kernel<D, false, NW, true>),
+                     dim3((unsigned)std::min(blocks, kF32MaxGrid)), dim3(64 * NW), 0, s, q, k, v, c,
+                     o, lse, 1, 1, 0, 0, sl2, pk);
+}
+
+hipError_t launch_packed_fwd_f32(const float* q, const float* k, const float* v, const float* c,
+                                 float* o, float* lse, const void* plan, int B, int H, int Hkv,
+                                 int N, int d, float scale, hipStream_t s) {
+  const F32Packed pk{static_cast<const PackedItem*>(plan), packed_items(B, N), H, Hkv, N};
+  if (d == 128) packed_fwd_f32_t<128, 4>(q, k, v, c, o, lse, pk, scale * kLog2e, s);
+  else packed_fwd_f32_t<64, 8>(q, k, v, c, o, lse, pk, scale * kLog2e, s);
+  return hipGetLastError();
+}
+
+template <int D, int NW>
+static void packed_bwd_f32_t(const float* q, const float* k, const float* v, const float* c,
+                             const float* lse, const float* d_o, const float* delta, float* dq,
+                             float* dk, float* dv, float* dcq, float* dck, const F32Packed& pk,
+                             float scale, hipStream_t s) {
+  const long long q_blocks = 4LL * pk.n_items * pk.H, k_blocks = 4LL * pk.n_items * pk.Hkv;
+  auto kv = [&](auto kernel, int nw) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(k_blocks, kF32MaxGrid)), dim3(64 * nw), 0, s,
+                       q, k, v, c, lse, d_o, delta, dk, dv, dck, 1, 1, 0, 0, scale, scale * kLog2e,
+                       pk);
+  };
+  auto qs = [&](auto kernel, int nw) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(q_blocks, kF32MaxGrid)), dim3(64 * nw), 0, s,
+                       q, k, v, c, lse, d_o, delta, dq, dcq, 1, 1, 0, 0, scale, scale * kLog2e, pk);
+  };
+  if (k_blocks <= kF32FineGroups) kv(bwd_dkdv_f32_kernel<D, false, NW, true>, NW);
+  else kv(bwd_dkdv_f32_kernel<D, false, NW / 2, true>, NW / 2);
+  if (q_blocks <= kF32FineGroups) qs(bwd_dq_f32_kernel<D, false, NW, true>, NW);
+  else qs(bwd_dq_f32_kernel<D, false, NW / 2, true>, NW / 2);
+}
+
+hipError_t launch_packed_bwd_f32(const float* q, const float* k, const float* v, const float* c,
+                                 const float* o, const float* lse, const float* d_o, float* dq,
+                                 float* dk, float* dv, float* delta, float* dcq, float* dck,
+                                 const void* plan, int B, int H, int Hkv, int N, int d,
+                                 float scale, hipStream_t s) {
+  const hipError_t e = launch_bwd_delta(false, o, d_o, delta, H, N, d, s);
+  if (e != hipSuccess) return e;
+  const F32Packed pk{static_cast<const PackedItem*>(plan), packed_items(B, N), H, Hkv, N};
+  if (d == 128)
+    packed_bwd_f32_t<128, 4>(q, k, v, c, lse, d_o, delta, dq, dk, dv, dcq, dck, pk, scale, s);
+  else
+    packed_bwd_f32_t<64, 8>(q, k, v, c, lse, d_o, delta, dq, dk, dv, dcq, dck, pk, scale, s);
   return hipGetLastError();
 }
 

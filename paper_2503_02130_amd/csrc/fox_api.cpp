@@ -95,6 +95,14 @@ int cache_max_len(const fox_cache_t* c, int max_len) {
   return max_len <= 0 || max_len > cap ? cap : max_len;
 }
 
+fox_status_t check_packed(int B, int H, int H_kv, int N) {
+  if (B <= 0 || H <= 0 || H_kv <= 0 || N <= 0 || H % H_kv != 0) return FOX_ERR_SHAPE;
+  if ((long long)H * N > (1LL << 31) - 1) return FOX_ERR_SHAPE;
+  if ((long long)B * H > (1LL << 21)) return FOX_ERR_SHAPE;  // a workgroup each, 1024 threads
+  if ((long long)H * fox::packed_items(B, N) > kMaxWorkgroups) return FOX_ERR_SHAPE;
+  return FOX_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -914,6 +922,110 @@ fox_status_t fox_attn_cache(const fox_cache_t* cache, const void* q, const int* 
   if (need && (!workspace || workspace_bytes < need)) return FOX_ERR_WORKSPACE;
   return launch_status(fox::launch_attn_cache(s, q, seq_len, parent, n_new, o, lse, workspace, n,
                                               len, scale, stream));
+}
+
+size_t fox_packed_plan_bytes(int B, int N) {
+  return B <= 0 || N <= 0 ? 0 : (size_t)fox::packed_items(B, N) * 16;
+}
+
+fox_status_t fox_packed_plan(const int* cu_seqlens, int B, int N, void* plan, size_t plan_bytes,
+                    hipStream_t stream) {
+  if (!cu_seqlens || !plan) return FOX_ERR_NULL;
+  fox_status_t st = check_packed(B, 1, 1, N);
+  if (st) return st;
+  if (!all_aligned16({cu_seqlens, plan})) return FOX_ERR_ALIGN;
+  if (plan_bytes < fox_packed_plan_bytes(B, N)) return FOX_ERR_WORKSPACE;
+  return launch_status(fox::launch_packed_plan(cu_seqlens, B, N, plan, stream));
+}
+
+fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_logit,
+                           const int* cu_seqlens, float* c, int B, int H, int N,
+                           hipStream_t stream) {
+  if (!all_set({gate_logit, cu_seqlens, c})) return FOX_ERR_NULL;
+  fox_status_t st = check_packed(B, H, H, N);
+  if (st) return st;
+  if (!cache_dtype(gate_dtype)) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({gate_logit, cu_seqlens, c})) return FOX_ERR_ALIGN;
+  return launch_status(fox::launch_packed_prefix(gate_dtype == FOX_DTYPE_BF16, gate_logit,
+                                                 cu_seqlens, c, B, H, N, stream));
+}
+
+fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
+                        const float* c, const void* plan, void* o, float* lse, int B, int H,
+                        int H_kv, int N, int d, int max_len, float scale, hipStream_t stream) {
+  if (!all_set({q, k, v, c, plan, o, lse})) return FOX_ERR_NULL;
+  fox_status_t st = check_packed(B, H, H_kv, N);
+  if (st) return st;
+  if (d <= 0 || (long long)N * d * 4 >= (1LL << 31)) return FOX_ERR_SHAPE;
+  st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if (!all_aligned16({q, k, v, c, plan, o, lse})) return FOX_ERR_ALIGN;
+  const int len = max_len <= 0 || max_len > N ? N : max_len;
+  if (dtype == FOX_DTYPE_BF16)
+    return launch_status(fox::launch_packed_fwd(q, k, v, c, o, lse, plan, B, H, H_kv, N, d, len,
+                                                scale, stream));
+  return launch_status(fox::launch_packed_fwd_f32((const float*)q, (const float*)k,
+                                                  (const float*)v, c, (float*)o, lse, plan, B, H,
+                                                  H_kv, N, d, scale, stream));
+}
+
+size_t fox_attn_bwd_packed_workspace_bytes(int H, int N) {
+  if (check_packed(1, H, H, N)) return 0;
+  return (size_t)3 * H * N * sizeof(float) + 32;
+}
+
+fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
+                        const float* c, const void* o, const float* lse, const void* d_o,
+                        fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
+                        const void* plan, void* dq, void* dk, void* dv, void* d_logit,
+                        float* d_log_f, void* workspace, size_t workspace_bytes, int B, int H,
+                        int H_kv, int N, int d, int max_len, float scale, hipStream_t stream) {
+  if (!all_set({q, k, v, c, o, lse, d_o, gate_logit, cu_seqlens, plan, dq, dk, dv, d_logit}))
+    return FOX_ERR_NULL;
+  fox_status_t st = check_packed(B, H, H_kv, N);
+  if (st) return st;
+  if (d <= 0 || (long long)N * d * 4 >= (1LL << 31)) return FOX_ERR_SHAPE;
+  st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if (!cache_dtype(gate_dtype)) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({q, k, v, c, o, lse, d_o, gate_logit, cu_seqlens, plan, dq, dk, dv, d_logit,
+                      d_log_f, workspace}))
+    return FOX_ERR_ALIGN;
+  if (!workspace || workspace_bytes < fox_attn_bwd_packed_workspace_bytes(H, N))
+    return FOX_ERR_WORKSPACE;
+  const int len = max_len <= 0 || max_len > N ? N : max_len;
+  // delta, dc_q, dc_k, each on a 16-byte boundary
+  const size_t row = ((size_t)H * N + 3) & ~(size_t)3;
+  float* delta = static_cast<float*>(workspace);
+  float *dcq = delta + row, *dck = dcq + row;
+  hipError_t e;
+  if (dtype == FOX_DTYPE_BF16)
+    e = fox::launch_packed_bwd(q, k, v, c, o, lse, d_o, dq, dk, dv, delta, dcq, dck, plan, B, H,
+                               H_kv, N, d, len, scale, stream);
+  else
+    e = fox::launch_packed_bwd_f32((const float*)q, (const float*)k, (const float*)v, c,
+                                   (const float*)o, lse, (const float*)d_o, (float*)dq, (float*)dk,
+                                   (float*)dv, delta, dcq, dck, plan, B, H, H_kv, N, d, scale,
+                                   stream);
+  if (e == hipSuccess)
+    e = fox::launch_packed_gate_grad(gate_dtype == FOX_DTYPE_BF16, dcq, dck, gate_logit,
+                                     cu_seqlens, d_log_f, d_logit, B, H, N, stream);
+  return launch_status(e);
+}
+
+fox_status_t fox_packed_zero_behind(const fox_packed_rows_t* tensors, int n, const int* cu_seqlens,
+                           int B, int N, hipStream_t stream) {
+  if (!tensors || !cu_seqlens) return FOX_ERR_NULL;
+  if (n < 1 || n > fox::kZeroTensors || B <= 0 || N <= 0) return FOX_ERR_SHAPE;
+  fox::ZeroRows x[fox::kZeroTensors];
+  for (int i = 0; i < n; ++i) {
+    if (!tensors[i].x) return FOX_ERR_NULL;
+    if (tensors[i].heads <= 0 || tensors[i].row_bytes <= 0 || tensors[i].row_bytes % 2)
+      return FOX_ERR_SHAPE;
+    if (!aligned16(tensors[i].x)) return FOX_ERR_ALIGN;
+    x[i] = fox::ZeroRows{tensors[i].x, tensors[i].heads, tensors[i].row_bytes};
+  }
+  return launch_status(fox::launch_packed_zero(x, n, cu_seqlens, B, N, stream));
 }
 
 }  // extern "C"

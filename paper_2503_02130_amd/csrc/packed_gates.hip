@@ -1,0 +1,196 @@
+// Packed sequences: the work list of the attention kernels, the gate prefix and its gradient.
+//
+//   plan      the 128-row blocks of all sequences, most key tiles first (block m of a sequence
+//             attends to m + 1 blocks).  Item (s, m) goes to place
+//             sum_t max(0, n_t - m - 1) + #{t < s : n_t > m}, n_t the blocks of sequence t:
+//             a wave per m finds both by one pass over the lengths, so there is no sort and
+//             no atomic.
+//   prefix    c = the running sum of log sigmoid(logit) within each sequence, one workgroup
+//             per (head, sequence).
+//   gradient  d(logit)_l = sigmoid(-logit_l) sum_{i >= l} (dc_q_i + dc_k_i), the same from the
+//             sequence's end.
+//
+// The scans run in 64 bits and round once: c of a long sequence is thousands with
+// differences of neighbours that matter, and fp32 sums of it are several units off.  They
+// are short chains of a few barriers per 8192 rows, bound by latency.
+#include <algorithm>
+
+#include "fox_internal.h"
+#include "packed.h"
+
+namespace fox {
+
+constexpr int kPScanThreads = 1024;
+constexpr int kPScanPer = 8;
+constexpr int kPScanSegment = kPScanThreads * kPScanPer;
+
+// first row and length of sequence b, within [0, N)
+__device__ __forceinline__ void packed_range(const int* __restrict__ cu, int b, int N, int& start,
+                                             int& len) {
+  start = min(max(cu[b], 0), N);
+  len = max(min(cu[b + 1], N) - start, 0);
+}
+
+__global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict__ cu, int B, int N,
+                                                          PackedItem* __restrict__ items,
+                                                          int n_items) {
+  const int lane = threadIdx.x & 63;
+  const int m = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
+  long long before = 0, total = 0;
+  for (int s = lane; s < B; s += 64) {
+    int start, len;
+    packed_range(cu, s, N, start, len);
+    const int nb = (len + kPackedBlock - 1) / kPackedBlock;
+    before += max(0, nb - m - 1);
+    total += nb;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    before += __shfl_xor(before, off);
+    total += __shfl_xor(total, off);
+  }
+  for (int s0 = 0; s0 < B; s0 += 64) {
+    int start = 0, len = 0;
+    if (s0 + lane < B) packed_range(cu, s0 + lane, N, start, len);
+    const bool has = (len + kPackedBlock - 1) / kPackedBlock > m;
+    const uint64_t mask = __ballot(has);
+    const long long at = before + __popcll(mask & ((1ull << lane) - 1));
+    if (has && at < n_items) items[at] = PackedItem{start, len, m, s0 + lane};
+    before += __popcll(mask);
+  }
+  if (m == 0)
+    for (long long i = total + lane; i < n_items; i += 64) items[i] = PackedItem{0, 0, 0, -1};
+}
+
+template <typename T>
+__device__ __forceinline__ float gate_at(const T* p, size_t i) {
+  return (float)p[i];
+}
+
+// GRAD false: out = c from logits a; true: out = d(logit) from a = dc_q, b = dc_k, logits g,
+// and d(log f) if aux.
+template <bool GRAD, typename T>
+__global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
+    const float* __restrict__ dcq, const float* __restrict__ dck, const T* __restrict__ logit,
+    const int* __restrict__ cu, float* __restrict__ c, float* __restrict__ aux,
+    T* __restrict__ d_logit, int B, int H, int N) {
+  __shared__ double wave_total[kPScanThreads / 64];
+  const int b = (int)(blockIdx.x / H), h = (int)(blockIdx.x % H);
+  int start, L;
+  packed_range(cu, b, N, start, L);
+  const size_t base = (size_t)h * N + start;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double carry = 0.0;
+  for (int seg = 0; seg < L; seg += kPScanSegment) {
+    const int p0 = seg + threadIdx.x * kPScanPer;
+    // element e of the thread, in scan order, lies at row p0 + e, or L - 1 - p0 - e from the end
+    float x[kPScanPer];
+#pragma unroll
+    for (int e = 0; e < kPScanPer; ++e) {
+      x[e] = 0.0f;
+      if (p0 + e < L) {
+        const size_t at = base + (GRAD ? L - 1 - p0 - e : p0 + e);
+        if constexpr (GRAD) x[e] = dcq[at] + dck[at];
+        else x[e] = log_sigmoid(gate_at(logit, at));
+      }
+    }
+    double run[kPScanPer], sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < kPScanPer; ++e) {
+      sum += x[e];
+      run[e] = sum;
+    }
+    double incl = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const double y = __shfl_up(incl, off);
+      if (lane >= off) incl += y;
+    }
+    if (lane == 63) wave_total[wave] = incl;
+    __syncthreads();
+    double prior = carry + (incl - sum);
+#pragma unroll
+    for (int w = 0; w < kPScanThreads / 64; ++w) {
+      if (w < wave) prior += wave_total[w];
+      carry += wave_total[w];
+    }
+#pragma unroll
+    for (int e = 0; e < kPScanPer; ++e)
+      if (p0 + e < L) {
+        const size_t at = base + (GRAD ? L - 1 - p0 - e : p0 + e);
+        const float y = (float)(prior + run[e]);
+        if constexpr (GRAD) {
+          if (aux) aux[at] = y;
+          d_logit[at] = (T)(y / (1.0f + expf(gate_at(logit, at))));
+        } else {
+          c[at] = y;
+        }
+      }
+    __syncthreads();
+  }
+}
+
+int packed_items(int B, int N) { return N / kPackedBlock + std::min(B, N); }
+
+hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, hipStream_t s) {
+  const int waves = (N + kPackedBlock - 1) / kPackedBlock;
+  hipLaunchKernelGGL(packed_plan_kernel, dim3((waves + 3) / 4), dim3(256), 0, s, cu, B, N,
+                     (PackedItem*)plan, packed_items(B, N));
+  return hipGetLastError();
+}
+
+hipError_t launch_packed_prefix(bool bf16_, const void* logit, const int* cu, float* c, int B,
+                                int H, int N, hipStream_t s) {
+  const dim3 grid((unsigned)B * (unsigned)H), block(kPScanThreads);
+  if (bf16_)
+    hipLaunchKernelGGL((packed_scan_kernel<false, bf16>), grid, block, 0, s, nullptr, nullptr,
+                       (const bf16*)logit, cu, c, nullptr, nullptr, B, H, N);
+  else
+    hipLaunchKernelGGL((packed_scan_kernel<false, float>), grid, block, 0, s, nullptr, nullptr,
+                       (const float*)logit, cu, c, nullptr, nullptr, B, H, N);
+  return hipGetLastError();
+}
+
+hipError_t launch_packed_gate_grad(bool bf16_, const float* dcq, const float* dck,
+                                   const void* logit, const int* cu, float* d_log_f,
+                                   void* d_logit, int B, int H, int N, hipStream_t s) {
+  const dim3 grid((unsigned)B * (unsigned)H), block(kPScanThreads);
+  if (bf16_)
+    hipLaunchKernelGGL((packed_scan_kernel<true, bf16>), grid, block, 0, s, dcq, dck,
+                       (const bf16*)logit, cu, nullptr, d_log_f, (bf16*)d_logit, B, H, N);
+  else
+    hipLaunchKernelGGL((packed_scan_kernel<true, float>), grid, block, 0, s, dcq, dck,
+                       (const float*)logit, cu, nullptr, d_log_f, (float*)d_logit, B, H, N);
+  return hipGetLastError();
+}
+
+// Zeros in the rows behind the last sequence of up to kZeroTensors tensors [heads, N, row].
+struct ZeroList {
+  ZeroRows x[kZeroTensors];
+  int n;
+};
+__global__ __launch_bounds__(256) void packed_zero_kernel(ZeroList list, const int* __restrict__ cu,
+                                                          int B, int N) {
+  const int first = min(max(cu[B], 0), N);
+  for (int i = 0; i < list.n; ++i) {
+    // every tensor in its own type's pieces: 2 bytes divide any row
+    const ZeroRows z = list.x[i];
+    const long long per = (long long)(N - first) * (z.row_bytes / 2);
+    for (long long j = (long long)blockIdx.x * 256 + threadIdx.x; j < per * z.heads;
+         j += (long long)gridDim.x * 256) {
+      const long long h = j / per, at = j % per;
+      static_cast<uint16_t*>(z.p)[(h * N + first) * (z.row_bytes / 2) + at] = 0;
+    }
+  }
+}
+
+hipError_t launch_packed_zero(const ZeroRows* x, int n, const int* cu, int B, int N,
+                              hipStream_t s) {
+  ZeroList list;
+  list.n = n;
+  for (int i = 0; i < n; ++i) list.x[i] = x[i];
+  hipLaunchKernelGGL(packed_zero_kernel, dim3(256), dim3(256), 0, s, list, cu, B, N);
+  return hipGetLastError();
+}
+
+}  // namespace fox
