@@ -44,6 +44,8 @@ constexpr int kCaThreads = 64 * kCaWaves;
 constexpr int kCaTile = 32;                        // keys of a wave's tile
 constexpr int kCaRound = kCaWaves * kCaTile;       // keys of one turn of the waves
 constexpr float kCaSum = 256.0f;                   // a lane's tile sum above it rescales
+// Workgroups that the keys are split for (most = one split per 4 turns).
+constexpr long long kCaWant = 4096, kCrWant = 512;
 constexpr float kCaFloor = -1e30f;                 // the maximum before the first key
 
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
@@ -90,6 +92,93 @@ __device__ __forceinline__ uint64_t ancestors(const int* __restrict__ parent, in
   return bits;
 }
 
+// Operand `st` of the first product (16 keys, dims in the order of ca_dim) from a lane's
+// 16-byte pieces of its key.
+template <bool F8>
+__device__ __forceinline__ bf16x8 k_operand(const u32x4d* w, int st) {
+  if constexpr (F8) return e4m3_operand(w[st >> 1][2 * (st & 1)], w[st >> 1][2 * (st & 1) + 1]);
+  else return __builtin_bit_cast(bf16x8, w[st]);
+}
+// first of the eight dims that a lane of group grp holds in operand st
+template <bool F8>
+__device__ __forceinline__ int ca_dim(int st, int grp) {
+  return F8 ? 64 * (st >> 1) + 16 * grp + 8 * (st & 1) : 32 * st + 8 * grp;
+}
+
+// The scales of a lane's four keys: s log2(e) 2^ek for the scores, 2^ev for the weights (bf16
+// caches: one value and none).  The scales of keys that do not exist are whatever lies there:
+// from `valid` on they become 0, where the weights are 0 too.
+template <bool F8>
+struct CaScales {
+  float k[F8 ? 4 : 1], v[F8 ? 4 : 1];
+  __device__ __forceinline__ void set(uint32_t ke, uint32_t ve, float scale_log2, int valid) {
+    if constexpr (F8) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        k[j] = scale_log2 * e4m3_scale((ke >> (8 * j)) & 255u);
+        v[j] = j < valid ? e4m3_scale((ve >> (8 * j)) & 255u) : 0.0f;
+      }
+    } else {
+      k[0] = scale_log2;
+    }
+  }
+  __device__ __forceinline__ float ks(int j) const { return k[F8 ? j : 0]; }
+};
+
+// Scores in base 2 of a lane's four keys of a half.
+template <bool F8>
+__device__ __forceinline__ void ca_scores(float* u, const f32x4& s, const f32x4& c, float ci,
+                                          const CaScales<F8>& sc) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) u[j] = (ci - c[j]) * kLog2e + s[j] * sc.ks(j);
+}
+// The mask of a tile that holds keys from `valid` on, which do not exist, or new tokens (from
+// kk = 0 on), of which only ancestors are seen.
+__device__ __forceinline__ void ca_mask(float* u, int valid, int kk0, uint64_t anc) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int kk = kk0 + j;
+    const int seen = (int)(j < valid) & ((int)(kk < 0) | (int)((anc >> (kk & 63)) & 1));
+    u[j] = seen ? u[j] : -INFINITY;
+  }
+}
+
+// The weights of PC groups of eight scores against the running maximum, as operands of the
+// second product; only if a lane's sum exceeds 2^8 the maximum is taken and all is rescaled.
+template <bool F8, int NB, int PC>
+__device__ __forceinline__ void ca_softmax(const float* u, float& m, float& l, f32x4 (&o)[NB],
+                                           const CaScales<F8>* sc, bf16x8* pb) {
+  float p[8 * PC], sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8 * PC; ++e) {
+    p[e] = exp2_fast(u[e] - m);
+    sum += p[e];
+  }
+  if (__any(sum > kCaSum)) {
+    float mt = u[0];
+#pragma unroll
+    for (int e = 1; e < 8 * PC; ++e) mt = fmaxf(mt, u[e]);
+    const float m_new = fmaxf(m, group_max(mt));
+    const float alpha = exp2_fast(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) o[db] *= alpha;
+    sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8 * PC; ++e) {
+      p[e] = exp2_fast(u[e] - m_new);
+      sum += p[e];
+    }
+  }
+  l += sum;
+#pragma unroll
+  for (int e = 0; e < 8 * PC; ++e) {
+    if constexpr (F8) pb[e / 8][e % 8] = to_bf16(p[e] * sc[e / 4].v[e % 4]);
+    else pb[e / 8][e % 8] = to_bf16(p[e]);
+  }
+}
+
 template <int D, int RT>
 struct CaMerge {
   float o[kCaWaves][16][D + 4];  // one row tile at a time
@@ -97,7 +186,9 @@ struct CaMerge {
 };
 
 template <int D, bool F8, int RT>
-__global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
+__global__ __launch_bounds__(kCaThreads)
+__attribute__((amdgpu_waves_per_eu(D == 64 ? (RT == 1 ? 4 : 3) : (RT == 1 ? 3 : 2))))
+void attn_cache_kernel(
     CacheView cv, const bf16* __restrict__ Q, const int* __restrict__ seq_len,
     const int* __restrict__ parent, const int* __restrict__ n_new, bf16* __restrict__ O,
     float* __restrict__ LSE, float* __restrict__ part_o, float* __restrict__ part_ml, int n, int G,
@@ -128,7 +219,7 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
   const int cap = (int)cv.capacity();
   const int len = min(max(seq_len[b], 0), cap);
   const int nn = n_new ? max(0, min(n_new[b], n)) : n;
-  const int T = min(len + nn, cap);
+  const int T = __builtin_amdgcn_readfirstlane(min(len + nn, cap));
   const int k0 = split * chunk;
   const int k1 = split == nsplit - 1 ? T : min(T, k0 + chunk);
   if (nn == 0 || (k0 >= T && split > 0)) return;
@@ -156,9 +247,7 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
     const bf16* q = Q + (((size_t)b * cv.H + head[i]) * n + (row_ok[i] ? tok[i] : 0)) * D;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      // the dims in the order in which a lane's 16-byte pieces of K hold them
-      const int d0 = F8 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
-      qf[i][s] = *reinterpret_cast<const bf16x8*>(q + d0);
+      qf[i][s] = *reinterpret_cast<const bf16x8*>(q + ca_dim<F8>(s, grp));
     }
   }
 
@@ -185,19 +274,20 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
   // The page numbers of a tile's halves, looked up one tile before its loads are issued.
   auto lookup = [&](int key0, int (&pg)[2]) {
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) pg[hf] = cv.page_of(b, key0 + 16 * hf);
+    for (int hf = 0; hf < 2; ++hf) pg[hf] = cv.page_entry(b, key0 + 16 * hf);
   };
   auto issue = [&](int key0, const int (&pg)[2], Tile& t) {
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       const int key = key0 + 16 * hf;
-      const int p = __builtin_amdgcn_readfirstlane(pg[hf]);
+      const bool there = cv.page_exists(pg[hf]) && key < T;
+      const int p = __builtin_amdgcn_readfirstlane(there ? pg[hf] : 0);
       const int slot = cv.slot_of(key);
-      t.valid[hf] = p < 0 ? 0 : max(0, min(16, T - key));
-      const size_t row = cv.kv_row(max(p, 0), hk, slot);
+      t.valid[hf] = there ? min(16, T - key) : 0;
+      const size_t row = cv.kv_row(p, hk, slot);
       const uint32_t bytes = (uint32_t)t.valid[hf] * D * ESZ;
-      const __amdgpu_buffer_rsrc_t rk = make_rsrc(static_cast<const char*>(cv.k) + row * (D * ESZ), bytes);
-      const __amdgpu_buffer_rsrc_t rv = make_rsrc(static_cast<const char*>(cv.v) + row * (D * ESZ), bytes);
+      const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(static_cast<const char*>(cv.k) + row * (D * ESZ), bytes);
+      const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(static_cast<const char*>(cv.v) + row * (D * ESZ), bytes);
 #pragma unroll
       for (int i = 0; i < KL; ++i)
         t.h[hf].k[i] = __builtin_bit_cast(
@@ -205,7 +295,7 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
 #pragma unroll
       for (int i = 0; i < RT; ++i)
         t.h[hf].c[i] = *reinterpret_cast<const f32x4*>(
-            cv.c + cv.c_at(max(p, 0), head[i], slot) + 4 * grp);
+            cv.c + cv.c_at(p, head[i], slot) + 4 * grp);
       if constexpr (F8) {
         t.h[hf].ke = *reinterpret_cast<const uint32_t*>(cv.ke + row + 4 * grp);
         t.h[hf].ve = *reinterpret_cast<const uint32_t*>(cv.ve + row + 4 * grp);
@@ -237,7 +327,10 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
     return (const lds_byte*)(uintptr_t)((uint32_t)(uintptr_t)lds_ptr(p) ^ (uint32_t)x);
   };
 
-  Tile cur, nxt;
+  // A tile's registers and LDS are refilled as soon as they have been read, before the second
+  // product: half the registers of a second set, so twice the waves, which hide more of the
+  // latency than the set did.
+  Tile cur;
   const int first = k0 + wave * kCaTile;
   int pg[2];
   lookup(first, pg);
@@ -246,7 +339,6 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
   for (int key0 = first; key0 < k1; key0 += kCaRound) {
     wait_all_memory();
     sched_fence();
-    // V of this tile to registers; then the next tile may overwrite it
     bf16x8 va[F8 ? 1 : NB];
     i32x2 v8[F8 ? NB : 1];
 #pragma unroll
@@ -259,11 +351,6 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
         va[db] = cat4(lo, hi);
       }
     }
-    wait_lds();
-    sched_fence();
-    if (key0 + kCaRound < k1) issue(key0 + kCaRound, pg, nxt);
-    lookup(key0 + 2 * kCaRound, pg);
-    sched_fence();
 
     // S^T of the two halves
     f32x4 s[RT][2];
@@ -273,77 +360,37 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
       for (int i = 0; i < RT; ++i) s[i][hf] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < NS; ++st) {
-        bf16x8 ka;
-        if constexpr (F8) {
-          const u32x4d w = cur.h[hf].k[st >> 1];
-          ka = e4m3_operand(w[2 * (st & 1)], w[2 * (st & 1) + 1]);
-        } else {
-          ka = __builtin_bit_cast(bf16x8, cur.h[hf].k[st]);
-        }
+        const bf16x8 ka = k_operand<F8>(cur.h[hf].k, st);
 #pragma unroll
         for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, qf[i][st], s[i][hf]);
       }
     }
     const bool plain = cur.valid[0] == 16 && cur.valid[1] == 16 && key0 + kCaTile <= len;
-    float ks[2][4], vs[2][4];
+    bf16x8 pb[RT];
+    CaScales<F8> sc[2];
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
+      sc[hf].set(cur.h[hf].ke, cur.h[hf].ve, scale_log2, plain ? 16 : cur.valid[hf] - 4 * grp);
+    float u[RT][8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        ks[hf][j] = scale_log2;
-        vs[hf][j] = 1.0f;
-        if constexpr (F8) {
-          ks[hf][j] = scale_log2 * e4m3_scale((cur.h[hf].ke >> (8 * j)) & 255u);
-          vs[hf][j] = e4m3_scale((cur.h[hf].ve >> (8 * j)) & 255u);
-          // keys that do not exist: their scales are whatever lies there
-          if (!plain && 4 * grp + j >= cur.valid[hf]) vs[hf][j] = 0.0f;
-        }
-      }
-    // weights of each row tile and O^T += V^T P^T
-    bf16x8 pb[RT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      float u[8];
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
+        ca_scores<F8>(u[i] + 4 * hf, s[i][hf], cur.h[hf].c[i], ci[i], sc[hf]);
+    if (!plain)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float x = (ci[i] - cur.h[hf].c[i][j]) * kLog2e + s[i][hf][j] * ks[hf][j];
-          if (!plain) {
-            const int kk = key0 + 16 * hf + 4 * grp + j - len;
-            const bool seen = row_ok[i] && 4 * grp + j < cur.valid[hf] &&
-                              (kk < 0 || ((anc[i] >> (kk & 63)) & 1) != 0);
-            if (!seen) x = -INFINITY;
-          }
-          u[4 * hf + j] = x;
-        }
-      float p[8], sum = 0.0f;
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = exp2_fast(u[e] - m[i]);
-        sum += p[e];
-      }
-      if (__any(sum > kCaSum)) {
-        float mt = u[0];
+        for (int hf = 0; hf < 2; ++hf)
+          ca_mask(u[i] + 4 * hf, row_ok[i] ? cur.valid[hf] - 4 * grp : 0,
+                  key0 + 16 * hf + 4 * grp - len, anc[i]);
 #pragma unroll
-        for (int e = 1; e < 8; ++e) mt = fmaxf(mt, u[e]);
-        const float m_new = fmaxf(m[i], group_max(mt));
-        const float alpha = exp2_fast(m[i] - m_new);
-        m[i] = m_new;
-        l[i] *= alpha;
-#pragma unroll
-        for (int db = 0; db < NB; ++db) oacc[i][db] *= alpha;
-        sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = exp2_fast(u[e] - m_new);
-          sum += p[e];
-        }
-      }
-      l[i] += sum;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pb[i][e] = to_bf16(p[e] * vs[e >> 2][e & 3]);
-    }
+    for (int i = 0; i < RT; ++i) ca_softmax<F8, NB, 1>(u[i], m[i], l[i], oacc[i], sc, &pb[i]);
+    sched_fence();
+    wait_lds();  // V is in registers
+    if (key0 + kCaRound < k1) issue(key0 + kCaRound, pg, cur);
+    lookup(key0 + 2 * kCaRound, pg);
+    sched_fence();
 #pragma unroll
     for (int db = 0; db < NB; ++db) {
       bf16x8 v;
@@ -352,7 +399,6 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
 #pragma unroll
       for (int i = 0; i < RT; ++i) oacc[i][db] = mfma16(v, pb[i], oacc[i][db]);
     }
-    cur = nxt;
   }
 
   // merge the waves
@@ -408,6 +454,310 @@ __global__ __launch_bounds__(kCaThreads) void attn_cache_kernel(
       }
     }
     if (i + 1 < RT) __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows (trees, large groups): the four waves of a workgroup own RT row tiles each and
+// walk the same 64-key tiles, K and V of which pass through LDS once for all of them, moved by
+// DMA and double-buffered, wave w moving the w-th 16 keys.  One barrier per tile; a wave's
+// rows are its own, so nothing is merged at the end.
+// ---------------------------------------------------------------------------
+constexpr int kCrTile = 64;
+
+// Place of a 16-byte piece of K in its row: the 16 keys of a half whose pieces one operand
+// read touches lie in different banks.
+template <int D, bool F8>
+__device__ __forceinline__ int k_swizzle(int key) {
+  constexpr int BYTES = D * (F8 ? 1 : 2);
+  return BYTES == 256 ? key & 15 : BYTES == 128 ? (key >> 1) & 7 : (key >> 2) & 3;
+}
+
+// transposing read of 8-bit elements at a byte address, as ds_read_tr_asm; valid after
+// lds_wait8()
+template <int OFF>
+__device__ __forceinline__ i32x2 ds_read_tr8_asm(uint32_t base) {
+  i32x2 r;
+  asm volatile("ds_read_b64_tr_b8 %0, %1 offset:%2" : "=v"(r) : "v"(base), "i"(OFF));
+  return r;
+}
+template <int N, int M>
+__device__ __forceinline__ void lds_wait8(i32x2 (&r)[M]) {
+  asm volatile("s_waitcnt lgkmcnt(%0)" ::"i"(N));
+#pragma unroll
+  for (int i = 0; i < M; ++i) asm volatile("" : "+v"(r[i]));
+}
+
+template <int D, bool F8>
+struct CrSmem {
+  char k[2][kCrTile * D * (F8 ? 1 : 2)];
+  char v[2][kCrTile * D * (F8 ? 1 : 2)];
+};
+
+template <int D, bool F8, int RT>
+__global__ __launch_bounds__(kCaThreads) __attribute__((amdgpu_waves_per_eu(2)))
+void attn_cache_rows_kernel(
+    CacheView cv, const bf16* __restrict__ Q, const int* __restrict__ seq_len,
+    const int* __restrict__ parent, const int* __restrict__ n_new, bf16* __restrict__ O,
+    float* __restrict__ LSE, float* __restrict__ part_o, float* __restrict__ part_ml, int n, int G,
+    int n_rowblk, int chunk, int nsplit, float scale_log2) {
+  constexpr int ESZ = F8 ? 1 : 2;
+  constexpr int ROW = D * ESZ, CPR = ROW / 16;
+  constexpr int KL = ROW / 64;           // 16-byte operand pieces of a lane per half
+  constexpr int NS = D / 32, NB = D / 16;
+  constexpr int HL = 16 * ROW / 1024;    // DMA loads of a half
+  constexpr int TB = kCrTile * ROW;      // bytes of a tile of K or V
+  __shared__ __attribute__((aligned(1024))) CrSmem<D, F8> sm;
+
+  const int nbase = cv.B * cv.Hkv * nsplit;
+  const int base = (int)(blockIdx.x / (8u * n_rowblk)) * 8 + (int)(blockIdx.x % 8u);
+  const int rb = (int)(blockIdx.x / 8u) % n_rowblk;
+  if (base >= nbase) return;
+  const int hk = base % cv.Hkv, b = base / cv.Hkv % cv.B, split = base / cv.Hkv / cv.B;
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int cap = (int)cv.capacity();
+  const int len = min(max(seq_len[b], 0), cap);
+  const int nn = n_new ? max(0, min(n_new[b], n)) : n;
+  const int T = __builtin_amdgcn_readfirstlane(min(len + nn, cap));
+  const int k0 = split * chunk;
+  const int k1 = split == nsplit - 1 ? T : min(T, k0 + chunk);
+  if (nn == 0 || (k0 >= T && split > 0)) return;
+
+  int head[RT];
+  bool row_ok[RT];
+  float ci[RT];
+  uint64_t anc[RT];
+  size_t out[RT];  // the row in O and LSE; of a row that is not there, unused
+  bool mine[RT];
+  bf16x8 qf[RT][NS];
+  const uint64_t bits = k1 > len ? ancestors(parent ? parent + (size_t)b * n : nullptr, nn, lane) : 0;
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const int r = ((rb * kCaWaves + wave) * RT + i) * 16 + col;
+    const int g = r / n, tok = r - g * n;
+    mine[i] = g < G && tok < nn;
+    head[i] = hk * G + (mine[i] ? g : 0);
+    const int own = mine[i] && len + tok < cap ? cv.page_of(b, len + tok) : -1;
+    row_ok[i] = own >= 0;
+    ci[i] = own < 0 ? -INFINITY : cv.c[cv.c_at(own, head[i], cv.slot_of(len + tok))];
+    const uint32_t lo = __shfl((uint32_t)bits, tok), hi = __shfl((uint32_t)(bits >> 32), tok);
+    anc[i] = ((uint64_t)hi << 32) | lo;
+    out[i] = ((size_t)b * cv.H + head[i]) * n + (mine[i] ? tok : 0);
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      qf[i][s] = *reinterpret_cast<const bf16x8*>(Q + out[i] * D + ca_dim<F8>(s, grp));
+  }
+  f32x4 oacc[RT][NB];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    m[i] = kCaFloor;
+    l[i] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // K and V of a tile to LDS: a wave moves its own 16 keys.  The lane's source offsets are
+  // formed anew for each tile (a few operations; kept, they would be spilled).
+  auto issue_kv = [&](int key0, int entry, auto bufc) {
+    constexpr int B = decltype(bufc)::value;
+    const int key = key0 + 16 * wave;
+    const bool there = cv.page_exists(entry) && key < T;
+    const size_t row = cv.kv_row(there ? entry : 0, hk, cv.slot_of(key));
+    const uint32_t bytes = there ? (uint32_t)min(16, T - key) * ROW : 0u;
+    const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(static_cast<const char*>(cv.k) + row * ROW, bytes);
+    const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(static_cast<const char*>(cv.v) + row * ROW, bytes);
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+#pragma unroll
+    for (int i = 0; i < HL; ++i) {
+      const int sl = i * 64 + ln, kr = sl / CPR, pc = sl % CPR;
+      dma16(rk, sm.k[B] + wave * 16 * ROW + i * 1024,
+            (uint32_t)(kr * ROW + 16 * (pc ^ k_swizzle<D, F8>(kr))));
+      dma16(rv, sm.v[B] + wave * 16 * ROW + i * 1024,
+            (uint32_t)(kr * ROW + 16 * (pc ^ v_swizzle<D, F8>(16 * (wave & 1) + kr))));
+    }
+  };
+  // what a wave keeps of a tile in registers: the prefix values and scales of its lanes' keys,
+  // refilled once the scores have been formed
+  struct Tile {
+    f32x4 c[4][RT];
+    uint32_t ke[4], ve[4];
+    int valid[4];
+  };
+  auto lookup = [&](int key0, int (&pg)[4]) {
+#pragma unroll
+    for (int hf = 0; hf < 4; ++hf) pg[hf] = cv.page_entry(b, key0 + 16 * hf);
+  };
+  auto issue_c = [&](int key0, const int (&pg)[4], Tile& t) {
+#pragma unroll
+    for (int hf = 0; hf < 4; ++hf) {
+      const int key = key0 + 16 * hf, slot = cv.slot_of(key);
+      const bool there = cv.page_exists(pg[hf]) && key < T;
+      const int p = __builtin_amdgcn_readfirstlane(there ? pg[hf] : 0);
+      t.valid[hf] = there ? min(16, T - key) : 0;
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+        t.c[hf][i] = *reinterpret_cast<const f32x4*>(cv.c + cv.c_at(p, head[i], slot) + 4 * grp);
+      if constexpr (F8) {
+        const size_t row = cv.kv_row(p, hk, slot);
+        t.ke[hf] = *reinterpret_cast<const uint32_t*>(cv.ke + row + 4 * grp);
+        t.ve[hf] = *reinterpret_cast<const uint32_t*>(cv.ve + row + 4 * grp);
+      }
+    }
+  };
+
+  // LDS addresses of the operand reads, opaque: the compiler then adds no wait for the tile
+  // that is loading into the other buffer
+  const lds_byte* kat[KL];
+#pragma unroll
+  for (int i = 0; i < KL; ++i)
+    kat[i] = lds_opaque(lds_ptr(&sm.k[0][0]) + col * ROW + 16 * ((4 * i + grp) ^ k_swizzle<D, F8>(col)));
+  uint32_t vat[2][NB];
+#pragma unroll
+  for (int db = 0; db < NB; ++db) {
+    if constexpr (F8) {
+      const int r8 = col >> 1, key = (r8 < 4 ? 0 : 12) + 4 * grp + r8;
+      vat[0][db] = lds_addr(&sm.v[0][0]) +
+                   (uint32_t)(key * ROW + 16 * (db ^ v_swizzle<D, F8>(key)) + 8 * (col & 1));
+      vat[1][db] = vat[0][db];
+    } else {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const int key = 16 * hf + 4 * grp + (col >> 2);
+        vat[hf][db] = lds_addr(&sm.v[0][0]) +
+                      (uint32_t)(key * ROW + 16 * ((2 * db + ((col >> 1) & 1)) ^ v_swizzle<D, F8>(key)) +
+                                 8 * (col & 1));
+      }
+    }
+  }
+
+  Tile t;
+  int pg[4];  // the next tile's pages
+  auto body = [&](int key0, auto bufc) {
+    constexpr int B = decltype(bufc)::value;
+    f32x4 s[RT][4];
+#pragma unroll
+    for (int hf = 0; hf < 4; ++hf) {
+      u32x4d kw[KL];
+#pragma unroll
+      for (int i = 0; i < KL; ++i)
+        kw[i] = __builtin_bit_cast(u32x4d, *(const lds_f32x4_t*)(kat[i] + B * TB + hf * 16 * ROW));
+#pragma unroll
+      for (int i = 0; i < RT; ++i) s[i][hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        const bf16x8 ka = k_operand<F8>(kw, st);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, qf[i][st], s[i][hf]);
+      }
+    }
+    const bool plain = key0 + kCrTile <= len && t.valid[0] == 16 && t.valid[1] == 16 &&
+                       t.valid[2] == 16 && t.valid[3] == 16;
+    CaScales<F8> sc[4];
+#pragma unroll
+    for (int hf = 0; hf < 4; ++hf)
+      sc[hf].set(t.ke[hf], t.ve[hf], scale_log2, plain ? 16 : t.valid[hf] - 4 * grp);
+    bf16x8 pb[RT][2];
+    float u[RT][16];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int hf = 0; hf < 4; ++hf)
+        ca_scores<F8>(u[i] + 4 * hf, s[i][hf], t.c[hf][i], ci[i], sc[hf]);
+    if (!plain)
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int hf = 0; hf < 4; ++hf)
+          ca_mask(u[i] + 4 * hf, row_ok[i] ? t.valid[hf] - 4 * grp : 0,
+                  key0 + 16 * hf + 4 * grp - len, anc[i]);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) ca_softmax<F8, NB, 2>(u[i], m[i], l[i], oacc[i], sc, pb[i]);
+    sched_fence();
+    if (key0 + kCrTile < k1) issue_c(key0 + kCrTile, pg, t);
+    lookup(key0 + 2 * kCrTile, pg);
+    sched_fence();
+    static_for<2>([&](auto pc) {
+      constexpr int P = decltype(pc)::value;  // 32 keys
+      constexpr int OFF = B * TB + P * 32 * ROW;
+      if constexpr (F8) {
+        i32x2 w[NB];
+#pragma unroll
+        for (int db = 0; db < NB; ++db) w[db] = ds_read_tr8_asm<OFF>(vat[0][db]);
+        lds_wait8<0>(w);
+#pragma unroll
+        for (int db = 0; db < NB; ++db) {
+          const bf16x8 v = e4m3_operand((uint32_t)w[db][0], (uint32_t)w[db][1]);
+#pragma unroll
+          for (int i = 0; i < RT; ++i) oacc[i][db] = mfma16(v, pb[i][P], oacc[i][db]);
+        }
+      } else {
+        bf16x4 w[2 * NB];
+#pragma unroll
+        for (int db = 0; db < NB; ++db) {
+          w[2 * db] = ds_read_tr_asm<OFF>(vat[0][db]);
+          w[2 * db + 1] = ds_read_tr_asm<OFF>(vat[1][db]);
+        }
+        lds_wait<0>(w);
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+            oacc[i][db] = mfma16(cat4(w[2 * db], w[2 * db + 1]), pb[i][P], oacc[i][db]);
+      }
+    });
+  };
+
+  lookup(k0, pg);
+  int own = cv.page_entry(b, k0 + 16 * wave);
+  if (k0 < k1) {
+    issue_kv(k0, own, std::integral_constant<int, 0>());
+    issue_c(k0, pg, t);
+  }
+  lookup(k0 + kCrTile, pg);
+  own = cv.page_entry(b, k0 + kCrTile + 16 * wave);
+  auto step = [&](int key0, auto bufc) {
+    constexpr int B = decltype(bufc)::value;
+    wait_all_memory();
+    __syncthreads();  // the tile is in LDS and everybody is done with the one before it
+    if (key0 + kCrTile < k1) issue_kv(key0 + kCrTile, own, std::integral_constant<int, 1 - B>());
+    own = cv.page_entry(b, key0 + 2 * kCrTile + 16 * wave);
+    sched_fence();
+    body(key0, bufc);
+  };
+  for (int key0 = k0; key0 < k1; key0 += 2 * kCrTile) {
+    step(key0, std::integral_constant<int, 0>());
+    if (key0 + kCrTile < k1) step(key0 + kCrTile, std::integral_constant<int, 1>());
+  }
+
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const float lt = group_sum(l[i]);
+    if (!mine[i]) continue;
+    if (nsplit == 1) {
+      const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;  // a row without a key: zeros, -inf
+#pragma unroll
+      for (int db = 0; db < NB; ++db) {
+        bf16x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = to_bf16(oacc[i][db][j] * inv);
+        *reinterpret_cast<bf16x4*>(O + out[i] * D + 16 * db + 4 * grp) = w;
+      }
+      if (grp == 0) LSE[out[i]] = lt > 0.0f ? kLn2 * (m[i] + log2f(lt)) : -INFINITY;
+    } else {
+      const size_t at = (size_t)split * cv.B * cv.H * n + out[i];
+#pragma unroll
+      for (int db = 0; db < NB; ++db)
+        *reinterpret_cast<f32x4*>(part_o + at * D + 16 * db + 4 * grp) = oacc[i][db];
+      if (grp == 0) {
+        part_ml[2 * at] = m[i];
+        part_ml[2 * at + 1] = lt;
+      }
+    }
   }
 }
 
@@ -467,18 +817,22 @@ __global__ __launch_bounds__(D / 4 * SG) void attn_cache_join_kernel(
 // launcher
 // ---------------------------------------------------------------------------
 struct CaPlan {
+  bool shared;  // the kernel for many rows
   int rt, n_rowblk, chunk, nsplit;
 };
 static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
   CaPlan p;
   const int rows = s.H / s.Hkv * n;
-  p.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  p.n_rowblk = (rows + 16 * p.rt - 1) / (16 * p.rt);
+  p.shared = rows > 32;
+  p.rt = p.shared ? (rows <= 64 ? 1 : 2) : rows <= 16 ? 1 : 2;
+  const int per = 16 * p.rt * (p.shared ? kCaWaves : 1);
+  p.n_rowblk = (rows + per - 1) / per;
+  const int unit = p.shared ? kCrTile : kCaRound;
   const long long base = (long long)s.B * s.Hkv * p.n_rowblk;
-  const long long most = std::max(1, (max_len + 2 * kCaRound - 1) / (2 * kCaRound));
-  const long long want = std::max<long long>(1, 1024 / base);
+  const long long most = std::max(1, (max_len + 4 * unit - 1) / (4 * unit));
+  const long long want = std::max<long long>(1, (p.shared ? kCrWant : kCaWant) / base);
   const long long ns = std::min(most, want);
-  p.chunk = (int)(((max_len + ns - 1) / ns + kCaRound - 1) / kCaRound * kCaRound);
+  p.chunk = (int)(((max_len + ns - 1) / ns + unit - 1) / unit * unit);
   p.nsplit = (int)((max_len + p.chunk - 1) / p.chunk);
   return p;
 }
@@ -497,16 +851,21 @@ hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_l
   float* part_ml = part_o + (size_t)p.nsplit * rows * s.d;
   const unsigned nbase = (unsigned)s.B * s.Hkv * p.nsplit;
   const dim3 grid((nbase + 7) / 8 * 8 * (unsigned)p.n_rowblk);
-  auto run = [&](auto dc, auto f8, auto rt) {
-    hipLaunchKernelGGL((attn_cache_kernel<decltype(dc)::value, decltype(f8)::value, decltype(rt)::value>),
-                       grid, dim3(kCaThreads), 0, st, cache_view(s), (const bf16*)q, seq_len, parent,
-                       n_new, (bf16*)o, lse, part_o, part_ml, n, s.H / s.Hkv, p.n_rowblk, p.chunk,
-                       p.nsplit, scale * kLog2e);
+  auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kCaThreads), 0, st, cache_view(s), (const bf16*)q, seq_len,
+                       parent, n_new, (bf16*)o, lse, part_o, part_ml, n, s.H / s.Hkv, p.n_rowblk,
+                       p.chunk, p.nsplit, scale * kLog2e);
   };
   auto by_rows = [&](auto dc, auto f8) {
-    if (p.rt == 1) run(dc, f8, std::integral_constant<int, 1>());
-    else if (p.rt == 2) run(dc, f8, std::integral_constant<int, 2>());
-    else run(dc, f8, std::integral_constant<int, 4>());
+    constexpr int D = decltype(dc)::value;
+    constexpr bool F8 = decltype(f8)::value;
+    if (p.shared) {
+      if (p.rt == 1) run(attn_cache_rows_kernel<D, F8, 1>);
+      else run(attn_cache_rows_kernel<D, F8, 2>);
+    } else {
+      if (p.rt == 1) run(attn_cache_kernel<D, F8, 1>);
+      else run(attn_cache_kernel<D, F8, 2>);
+    }
   };
   auto by_format = [&](auto dc) {
     if (s.f8) by_rows(dc, std::true_type());

@@ -26,6 +26,14 @@ struct CacheView {
     const int p = table[(size_t)b * max_pages + i];
     return (unsigned)p < (unsigned)n_pages ? p : -1;
   }
+  // The table's entry for position pos (of the table's last place, past its end), unchecked,
+  // by a scalar load: pos is the same in the whole wave.  page_exists() says whether it is one.
+  __device__ int page_entry(int b, int pos) const {
+    typedef const __attribute__((address_space(4))) int table_t;
+    const int i = min(pos >> page_shift, max_pages - 1);
+    return ((table_t*)(uintptr_t)table)[(size_t)b * max_pages + i];
+  }
+  __device__ bool page_exists(int p) const { return (unsigned)p < (unsigned)n_pages; }
   __device__ int slot_of(int pos) const { return pos & ((1 << page_shift) - 1); }
   // index of (page p, key head h, slot) in k_exp and, times d, in k and v
   __device__ size_t kv_row(int p, int h, int slot) const {
@@ -42,6 +50,14 @@ inline CacheView cache_view(const CacheSpec& s) {
 }
 
 constexpr int kMaxNew = 64;  // new tokens of a sequence per call: a row's ancestors are 64 bits
+
+// A buffer descriptor whose parts are the same in the whole wave but that the compiler cannot
+// see to be (it would loop over the lanes' descriptors around every load).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const char* p, uint32_t bytes) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  const uint64_t u = ((uint64_t)uniform_u32((uint32_t)(a >> 32)) << 32) | uniform_u32((uint32_t)a);
+  return make_rsrc((const void*)(uintptr_t)u, uniform_u32(bytes));
+}
 
 // e4m3 rows share one scale 2^e, stored as the biased exponent e + 127.  It is the least
 // power of two, from 2^-126, that brings the row's largest magnitude to 448 or below.  A
