@@ -16,8 +16,11 @@
 //     rows r on its columns, so a lane owns one r) and O^T += V^T P^T, whose B operand is the
 //     P^T that the first product left in the registers; the key order of the contraction is
 //     the accumulator's, given to V alike.
-//   * Keys are split over the grid in chunks, and a workgroup's four waves take 32-key tiles
-//     in turn, each with its own running maximum and sum: no barrier in the loop.  K comes
+//   * Keys are split over the grid: all sequences' keys together are cut into about as many
+//     equal pieces as workgroups are wanted, each within one sequence, from the lengths on the
+//     device (ca_piece), so a batch of ragged lengths loads the part evenly.
+//   * A workgroup's four waves take 32-key tiles in turn, each with its own running maximum
+//     and sum: no barrier in the loop.  K comes
 //     straight into operand registers (a lane reads 16 bytes of a key); V passes through the
 //     wave's LDS by DMA and is read back transposed.  The next tile's loads are in flight
 //     while a tile is computed.
@@ -44,8 +47,9 @@ constexpr int kCaThreads = 64 * kCaWaves;
 constexpr int kCaTile = 32;                        // keys of a wave's tile
 constexpr int kCaRound = kCaWaves * kCaTile;       // keys of one turn of the waves
 constexpr float kCaSum = 256.0f;                   // a lane's tile sum above it rescales
-// Workgroups that the keys are split for (most = one split per 4 turns).
-constexpr long long kCaWant = 4096, kCrWant = 512;
+// Workgroups that the keys are split for, and the least units of keys of a piece.
+constexpr long long kCaWant = 2048, kCrWant = 512;
+constexpr int kCaMin = 2, kCrMin = 4;
 constexpr float kCaFloor = -1e30f;                 // the maximum before the first key
 
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
@@ -91,6 +95,78 @@ __device__ __forceinline__ uint64_t ancestors(const int* __restrict__ parent, in
   }
   return bits;
 }
+
+// What a workgroup takes of the keys: positions k0 .. k1 - 1 of sequence b, the split-th of its
+// `count` pieces, whose first is number `first` of all.
+struct CaPiece {
+  int b, len, nn, T, k0, k1, split, count, first;
+};
+struct CaSplit {
+  int unit;       // keys that a piece's length is a multiple of
+  int min_units;  // of a piece
+  int target;     // pieces wanted; 0: one of each sequence
+};
+// Piece number `piece`, found by every wave for itself from the lengths of the sequences: with
+// W units of keys in all, a piece has max(min_units, ceil(W / target)) units at most, so that
+// there are at most target + B of them whatever the lengths, and a sequence's pieces are
+// equal.  False: there are fewer pieces.
+__device__ __forceinline__ bool ca_piece(const CacheView& cv, const int* __restrict__ seq_len,
+                                         const int* __restrict__ n_new, int n, const CaSplit& sp,
+                                         int piece, int lane, CaPiece& out) {
+  const int cap = (int)cv.capacity();
+  auto units_of = [&](int b) {
+    if (b >= cv.B) return 0;
+    const int nn = n_new ? max(0, min(n_new[b], n)) : n;
+    const int T = min(min(max(seq_len[b], 0), cap) + nn, cap);
+    return nn == 0 ? 0 : (T + sp.unit - 1) / sp.unit;
+  };
+  long long total = 0;
+  for (int b0 = 0; b0 < cv.B; b0 += 64) {
+    long long u = units_of(b0 + lane);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) u += __shfl_xor(u, off);
+    total += u;
+  }
+  const int most = sp.target == 0 ? 1 << 30
+                                  : (int)max((long long)sp.min_units, (total + sp.target - 1) / sp.target);
+  int first = 0;
+  for (int b0 = 0; b0 < cv.B; b0 += 64) {
+    const int u = units_of(b0 + lane), pieces = u / most + (u % most != 0);
+    int incl = pieces;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(incl, off);
+      if (lane >= off) incl += y;
+    }
+    const uint64_t past = __ballot(first + incl > piece);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      const int b = b0 + l;
+      out.b = b;
+      out.count = __builtin_amdgcn_readlane(pieces, l);
+      out.first = first + __builtin_amdgcn_readlane(incl, l) - out.count;
+      out.split = piece - out.first;
+      out.len = min(max(seq_len[b], 0), cap);
+      out.nn = n_new ? max(0, min(n_new[b], n)) : n;
+      out.T = __builtin_amdgcn_readfirstlane(min(out.len + out.nn, cap));
+      const int units = __builtin_amdgcn_readlane(u, l);
+      const int per = (units + out.count - 1) / out.count * sp.unit;
+      out.k0 = out.split * per;
+      out.k1 = min(out.T, out.k0 + per);
+      return true;
+    }
+    first += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// Where the parts of split sequences meet: the first piece and the number of pieces of each
+// sequence, then O and (maximum, sum) of [piece][head of the key head's group, token] rows.
+struct CaParts {
+  int2* table;  // [B]
+  float* o;
+  float* ml;
+};
 
 // Operand `st` of the first product (16 keys, dims in the order of ca_dim) from a lane's
 // 16-byte pieces of its key.
@@ -191,8 +267,8 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? (RT == 1 ? 4 : 3) : (RT == 1 ? 3 : 
 void attn_cache_kernel(
     CacheView cv, const bf16* __restrict__ Q, const int* __restrict__ seq_len,
     const int* __restrict__ parent, const int* __restrict__ n_new, bf16* __restrict__ O,
-    float* __restrict__ LSE, float* __restrict__ part_o, float* __restrict__ part_ml, int n, int G,
-    int n_rowblk, int chunk, int nsplit, float scale_log2) {
+    float* __restrict__ LSE, CaParts parts, CaSplit sp, int n, int G, int n_rowblk, int n_pieces,
+    float scale_log2) {
   constexpr int ESZ = F8 ? 1 : 2;
   constexpr int CPR = D * ESZ / 16;                    // 16-byte pieces of a row
   constexpr int KL = D * ESZ / 64;                     // 16-byte K loads of a lane per half
@@ -207,22 +283,20 @@ void attn_cache_kernel(
   __shared__ __attribute__((aligned(1024))) Smem sm;
 
   // row blocks of the same keys follow each other on one XCD
-  const int nbase = cv.B * cv.Hkv * nsplit;
+  const int nbase = cv.Hkv * n_pieces;
   const int base = (int)(blockIdx.x / (8u * n_rowblk)) * 8 + (int)(blockIdx.x % 8u);
   const int rb = (int)(blockIdx.x / 8u) % n_rowblk;
   if (base >= nbase) return;
-  const int hk = base % cv.Hkv, b = base / cv.Hkv % cv.B, split = base / cv.Hkv / cv.B;
-
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, grp = lane >> 4;
+  const int hk = base % cv.Hkv;
+  CaPiece pc;
+  if (!ca_piece(cv, seq_len, n_new, n, sp, base / cv.Hkv, lane, pc)) return;
+  const int b = pc.b, len = pc.len, nn = pc.nn, T = pc.T, k0 = pc.k0, k1 = pc.k1;
   const int cap = (int)cv.capacity();
-  const int len = min(max(seq_len[b], 0), cap);
-  const int nn = n_new ? max(0, min(n_new[b], n)) : n;
-  const int T = __builtin_amdgcn_readfirstlane(min(len + nn, cap));
-  const int k0 = split * chunk;
-  const int k1 = split == nsplit - 1 ? T : min(T, k0 + chunk);
-  if (nn == 0 || (k0 >= T && split > 0)) return;
+  if (pc.split == 0 && hk == 0 && rb == 0 && threadIdx.x == 0 && parts.table)
+    parts.table[b] = make_int2(pc.first, pc.count);
+  const int col = lane & 15, grp = lane >> 4;
 
   // this lane's rows
   int head[RT], tok[RT];
@@ -437,7 +511,7 @@ void attn_cache_kernel(
         o += *reinterpret_cast<const f32x4*>(&sm.merge.o[w][rr][e]);
       }
       const size_t R = ((size_t)b * cv.H + hk * G + g) * n + t;
-      if (nsplit == 1) {
+      if (pc.count == 1) {
         const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;  // a row without a key: zeros, -inf
         bf16x4 w4;
 #pragma unroll
@@ -445,11 +519,11 @@ void attn_cache_kernel(
         *reinterpret_cast<bf16x4*>(O + R * D + e) = w4;
         if (e == 0) LSE[R] = lr > 0.0f ? kLn2 * (Mr + log2f(lr)) : -INFINITY;
       } else {
-        const size_t at = (size_t)split * cv.B * cv.H * n + R;
-        *reinterpret_cast<f32x4*>(part_o + at * D + e) = o;
+        const size_t at = ((size_t)(pc.first + pc.split) * cv.H + hk * G + g) * n + t;
+        *reinterpret_cast<f32x4*>(parts.o + at * D + e) = o;
         if (e == 0) {
-          part_ml[2 * at] = Mr;
-          part_ml[2 * at + 1] = lr;
+          parts.ml[2 * at] = Mr;
+          parts.ml[2 * at + 1] = lr;
         }
       }
     }
@@ -499,8 +573,8 @@ __global__ __launch_bounds__(kCaThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void attn_cache_rows_kernel(
     CacheView cv, const bf16* __restrict__ Q, const int* __restrict__ seq_len,
     const int* __restrict__ parent, const int* __restrict__ n_new, bf16* __restrict__ O,
-    float* __restrict__ LSE, float* __restrict__ part_o, float* __restrict__ part_ml, int n, int G,
-    int n_rowblk, int chunk, int nsplit, float scale_log2) {
+    float* __restrict__ LSE, CaParts parts, CaSplit sp, int n, int G, int n_rowblk, int n_pieces,
+    float scale_log2) {
   constexpr int ESZ = F8 ? 1 : 2;
   constexpr int ROW = D * ESZ, CPR = ROW / 16;
   constexpr int KL = ROW / 64;           // 16-byte operand pieces of a lane per half
@@ -509,22 +583,20 @@ void attn_cache_rows_kernel(
   constexpr int TB = kCrTile * ROW;      // bytes of a tile of K or V
   __shared__ __attribute__((aligned(1024))) CrSmem<D, F8> sm;
 
-  const int nbase = cv.B * cv.Hkv * nsplit;
+  const int nbase = cv.Hkv * n_pieces;
   const int base = (int)(blockIdx.x / (8u * n_rowblk)) * 8 + (int)(blockIdx.x % 8u);
   const int rb = (int)(blockIdx.x / 8u) % n_rowblk;
   if (base >= nbase) return;
-  const int hk = base % cv.Hkv, b = base / cv.Hkv % cv.B, split = base / cv.Hkv / cv.B;
-
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, grp = lane >> 4;
+  const int hk = base % cv.Hkv;
+  CaPiece pc;
+  if (!ca_piece(cv, seq_len, n_new, n, sp, base / cv.Hkv, lane, pc)) return;
+  const int b = pc.b, len = pc.len, nn = pc.nn, T = pc.T, k0 = pc.k0, k1 = pc.k1;
   const int cap = (int)cv.capacity();
-  const int len = min(max(seq_len[b], 0), cap);
-  const int nn = n_new ? max(0, min(n_new[b], n)) : n;
-  const int T = __builtin_amdgcn_readfirstlane(min(len + nn, cap));
-  const int k0 = split * chunk;
-  const int k1 = split == nsplit - 1 ? T : min(T, k0 + chunk);
-  if (nn == 0 || (k0 >= T && split > 0)) return;
+  if (pc.split == 0 && hk == 0 && rb == 0 && threadIdx.x == 0 && parts.table)
+    parts.table[b] = make_int2(pc.first, pc.count);
+  const int col = lane & 15, grp = lane >> 4;
 
   int head[RT];
   bool row_ok[RT];
@@ -738,7 +810,7 @@ void attn_cache_rows_kernel(
   for (int i = 0; i < RT; ++i) {
     const float lt = group_sum(l[i]);
     if (!mine[i]) continue;
-    if (nsplit == 1) {
+    if (pc.count == 1) {
       const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;  // a row without a key: zeros, -inf
 #pragma unroll
       for (int db = 0; db < NB; ++db) {
@@ -749,42 +821,41 @@ void attn_cache_rows_kernel(
       }
       if (grp == 0) LSE[out[i]] = lt > 0.0f ? kLn2 * (m[i] + log2f(lt)) : -INFINITY;
     } else {
-      const size_t at = (size_t)split * cv.B * cv.H * n + out[i];
+      // (piece, head, token): out[i] without its sequence
+      const size_t at = (size_t)(pc.first + pc.split - b) * cv.H * n + out[i];
 #pragma unroll
       for (int db = 0; db < NB; ++db)
-        *reinterpret_cast<f32x4*>(part_o + at * D + 16 * db + 4 * grp) = oacc[i][db];
+        *reinterpret_cast<f32x4*>(parts.o + at * D + 16 * db + 4 * grp) = oacc[i][db];
       if (grp == 0) {
-        part_ml[2 * at] = m[i];
-        part_ml[2 * at + 1] = lt;
+        parts.ml[2 * at] = m[i];
+        parts.ml[2 * at + 1] = lt;
       }
     }
   }
 }
 
-// The splits of a row joined: D / 4 lanes hold a row's elements, the lane groups of a
-// workgroup take every SG-th split and meet in LDS.
+// The pieces of a row joined: D / 4 lanes hold a row's elements, the lane groups of a
+// workgroup take every SG-th piece and meet in LDS.
 template <int D, int SG>
 __global__ __launch_bounds__(D / 4 * SG) void attn_cache_join_kernel(
-    const float* __restrict__ part_o, const float* __restrict__ part_ml,
-    const int* __restrict__ seq_len, const int* __restrict__ n_new, bf16* __restrict__ O,
-    float* __restrict__ LSE, int BH, int H, int n, int cap, int chunk, int nsplit) {
+    CaParts parts, const int* __restrict__ n_new, bf16* __restrict__ O, float* __restrict__ LSE,
+    int H, int n) {
   constexpr int LPR = D / 4;
   __shared__ float so[SG][D];
   __shared__ float sml[SG][2];
   const size_t R = blockIdx.x;
   const int t = (int)(R % n), b = (int)(R / n / H);
-  const int nn = n_new ? max(0, min(n_new[b], n)) : n;
-  if (t >= nn) return;
-  const int T = min(min(max(seq_len[b], 0), cap) + nn, cap);
-  const int ns = max(1, min(nsplit, (T + chunk - 1) / chunk));
-  const size_t stride = (size_t)BH * n;
+  if (t >= (n_new ? min(n_new[b], n) : n)) return;
+  const int2 pieces = parts.table[b];
+  if (pieces.y == 1) return;  // written by its only piece
+  const size_t stride = (size_t)H * n, row = (size_t)pieces.x * stride + R - (size_t)b * stride;
   const int part = threadIdx.x % LPR, sg = threadIdx.x / LPR;
   float M = kCaFloor, l = 0.0f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = sg; s < ns; s += SG) {
-    const size_t at = s * stride + R;
-    const float ms = part_ml[2 * at], ls = part_ml[2 * at + 1];
-    const f32x4 os = *reinterpret_cast<const f32x4*>(part_o + at * D + 4 * part);
+  for (int s = sg; s < pieces.y; s += SG) {
+    const size_t at = s * stride + row;
+    const float ms = parts.ml[2 * at], ls = parts.ml[2 * at + 1];
+    const f32x4 os = *reinterpret_cast<const f32x4*>(parts.o + at * D + 4 * part);
     const float Mn = fmaxf(M, ms);
     const float a = exp2_fast(M - Mn), f = exp2_fast(ms - Mn);
     o = o * a + os * f;
@@ -818,7 +889,8 @@ __global__ __launch_bounds__(D / 4 * SG) void attn_cache_join_kernel(
 // ---------------------------------------------------------------------------
 struct CaPlan {
   bool shared;  // the kernel for many rows
-  int rt, n_rowblk, chunk, nsplit;
+  int rt, n_rowblk, n_pieces;
+  CaSplit split;
 };
 static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
   CaPlan p;
@@ -827,19 +899,25 @@ static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
   p.rt = p.shared ? (rows <= 64 ? 1 : 2) : rows <= 16 ? 1 : 2;
   const int per = 16 * p.rt * (p.shared ? kCaWaves : 1);
   p.n_rowblk = (rows + per - 1) / per;
-  const int unit = p.shared ? kCrTile : kCaRound;
-  const long long base = (long long)s.B * s.Hkv * p.n_rowblk;
-  const long long most = std::max(1, (max_len + 4 * unit - 1) / (4 * unit));
-  const long long want = std::max<long long>(1, (p.shared ? kCrWant : kCaWant) / base);
-  const long long ns = std::min(most, want);
-  p.chunk = (int)(((max_len + ns - 1) / ns + unit - 1) / unit * unit);
-  p.nsplit = (int)((max_len + p.chunk - 1) / p.chunk);
+  p.split.unit = p.shared ? kCrTile : kCaRound;
+  p.split.min_units = p.shared ? kCrMin : kCaMin;
+  const long long want = (p.shared ? kCrWant : kCaWant) / ((long long)s.Hkv * p.n_rowblk);
+  p.split.target = (int)std::max<long long>(1, want);
+  // no more than sequences of max_len make, and none where each is one least piece; longer
+  // ones are then cut into larger pieces
+  const long long units = ((long long)max_len + p.split.unit - 1) / p.split.unit;
+  const long long each = (units + p.split.min_units - 1) / p.split.min_units;
+  p.split.target = each == 1 ? 0 : (int)std::min<long long>(p.split.target, each * s.B);
+  p.n_pieces = p.split.target + s.B;
   return p;
 }
+static size_t ca_table_bytes(int B) { return ((size_t)B * sizeof(int2) + 255) & ~(size_t)255; }
 
 size_t attn_cache_workspace_bytes(const CacheSpec& s, int n, int max_len) {
   const CaPlan p = ca_plan(s, n, max_len);
-  return p.nsplit == 1 ? 0 : (size_t)p.nsplit * s.B * s.H * n * (s.d + 2) * sizeof(float);
+  return p.n_pieces <= s.B ? 0
+                           : ca_table_bytes(s.B) +
+                                 (size_t)p.n_pieces * s.H * n * (s.d + 2) * sizeof(float);
 }
 
 hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_len,
@@ -847,14 +925,18 @@ hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_l
                              int n, int max_len, float scale, hipStream_t st) {
   const CaPlan p = ca_plan(s, n, max_len);
   const size_t rows = (size_t)s.B * s.H * n;
-  float* part_o = static_cast<float*>(ws);
-  float* part_ml = part_o + (size_t)p.nsplit * rows * s.d;
-  const unsigned nbase = (unsigned)s.B * s.Hkv * p.nsplit;
+  CaParts parts{};
+  if (p.n_pieces > s.B) {
+    parts.table = static_cast<int2*>(ws);
+    parts.o = reinterpret_cast<float*>(static_cast<char*>(ws) + ca_table_bytes(s.B));
+    parts.ml = parts.o + (size_t)p.n_pieces * s.H * n * s.d;
+  }
+  const unsigned nbase = (unsigned)s.Hkv * p.n_pieces;
   const dim3 grid((nbase + 7) / 8 * 8 * (unsigned)p.n_rowblk);
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(kCaThreads), 0, st, cache_view(s), (const bf16*)q, seq_len,
-                       parent, n_new, (bf16*)o, lse, part_o, part_ml, n, s.H / s.Hkv, p.n_rowblk,
-                       p.chunk, p.nsplit, scale * kLog2e);
+                       parent, n_new, (bf16*)o, lse, parts, p.split, n, s.H / s.Hkv, p.n_rowblk,
+                       p.n_pieces, scale * kLog2e);
   };
   auto by_rows = [&](auto dc, auto f8) {
     constexpr int D = decltype(dc)::value;
@@ -873,16 +955,13 @@ hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_l
   };
   if (s.d == 128) by_format(std::integral_constant<int, 128>());
   else by_format(std::integral_constant<int, 64>());
-  if (p.nsplit > 1) {
-    const int cap = (int)std::min<long long>((long long)s.max_pages * s.page, 0x7fffffff);
+  if (p.n_pieces > s.B) {
     if (s.d == 128)
       hipLaunchKernelGGL((attn_cache_join_kernel<128, 8>), dim3((unsigned)rows), dim3(256), 0, st,
-                         part_o, part_ml, seq_len, n_new, (bf16*)o, lse, s.B * s.H, s.H, n, cap,
-                         p.chunk, p.nsplit);
+                         parts, n_new, (bf16*)o, lse, s.H, n);
     else
       hipLaunchKernelGGL((attn_cache_join_kernel<64, 16>), dim3((unsigned)rows), dim3(256), 0, st,
-                         part_o, part_ml, seq_len, n_new, (bf16*)o, lse, s.B * s.H, s.H, n, cap,
-                         p.chunk, p.nsplit);
+                         parts, n_new, (bf16*)o, lse, s.H, n);
   }
   return hipGetLastError();
 }
