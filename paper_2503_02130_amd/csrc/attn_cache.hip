@@ -27,6 +27,8 @@
 //   * A tile of 32 keys is two halves of 16, each inside one page (pages hold 16 tokens or
 //     more); a half is addressed through a buffer descriptor that ends where its keys end, so
 //     nothing behind the sequence is read, and keys without a page read as zero and are masked.
+//   * Tiles are visited from the newest keys backwards: older ones are the more forgotten, so
+//     the first tile's maximum serves nearly all others.
 //   * Scores are exponentiated against the running maximum; only if a lane's sum of a tile
 //     exceeds 2^8 is the tile's maximum taken and everything rescaled (bf16 P and the fp32
 //     sums absorb the 8 bits).  The row sum adds the unrounded fp32 P, P V takes P rounded to
@@ -182,34 +184,44 @@ __device__ __forceinline__ int ca_dim(int st, int grp) {
 }
 
 // The scales of a lane's four keys: s log2(e) 2^ek for the scores, 2^ev for the weights (bf16
-// caches: one value and none).  The scales of keys that do not exist are whatever lies there:
-// from `valid` on they become 0, where the weights are 0 too.
+// caches: one value and none).
 template <bool F8>
 struct CaScales {
   float k[F8 ? 4 : 1], v[F8 ? 4 : 1];
-  __device__ __forceinline__ void set(uint32_t ke, uint32_t ve, float scale_log2, int valid) {
+  __device__ __forceinline__ void set(uint32_t ke, uint32_t ve, float scale_log2) {
     if constexpr (F8) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         k[j] = scale_log2 * e4m3_scale((ke >> (8 * j)) & 255u);
-        v[j] = j < valid ? e4m3_scale((ve >> (8 * j)) & 255u) : 0.0f;
+        v[j] = e4m3_scale((ve >> (8 * j)) & 255u);
       }
     } else {
       k[0] = scale_log2;
     }
   }
+  // The scales of keys that do not exist are whatever lies there; their weights are 0.
+  __device__ __forceinline__ void clear_from(int valid) {
+    if constexpr (F8) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = j < valid ? v[j] : 0.0f;
+    }
+  }
   __device__ __forceinline__ float ks(int j) const { return k[F8 ? j : 0]; }
 };
 
-// Scores in base 2 of a lane's four keys of a half.
+// Scores in base 2, less `base`, of a lane's four keys of a half.
 template <bool F8>
-__device__ __forceinline__ void ca_scores(float* u, const f32x4& s, const f32x4& c, float ci,
-                                          const CaScales<F8>& sc) {
+__device__ __forceinline__ void ca_scores(float* x, const f32x4& s, const f32x4& c, float ci,
+                                          const CaScales<F8>& sc, float base) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) u[j] = (ci - c[j]) * kLog2e + s[j] * sc.ks(j);
+  for (int j = 0; j < 4; ++j)
+    x[j] = __builtin_fmaf(s[j], sc.ks(j), __builtin_fmaf(ci - c[j], kLog2e, -base));
 }
-// The mask of a tile that holds keys from `valid` on, which do not exist, or new tokens (from
-// kk = 0 on), of which only ancestors are seen.
+// What the scores of a row are taken relative to: its running maximum, once it has seen a key.
+__device__ __forceinline__ float ca_base(float m) { return m == kCaFloor ? 0.0f : m; }
+
+// The mask of a lane's four keys of a half in a tile that holds keys from `valid` on, which do
+// not exist, or new tokens (from kk = 0 on), of which only ancestors are seen.
 __device__ __forceinline__ void ca_mask(float* u, int valid, int kk0, uint64_t anc) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -219,39 +231,63 @@ __device__ __forceinline__ void ca_mask(float* u, int valid, int kk0, uint64_t a
   }
 }
 
-// The weights of PC groups of eight scores against the running maximum, as operands of the
-// second product; only if a lane's sum exceeds 2^8 the maximum is taken and all is rescaled.
-template <bool F8, int NB, int PC>
-__device__ __forceinline__ void ca_softmax(const float* u, float& m, float& l, f32x4 (&o)[NB],
-                                           const CaScales<F8>* sc, bf16x8* pb) {
-  float p[8 * PC], sum = 0.0f;
+// The weights of one row's 4 NH scores (x, less ca_base(m)), as operands of the second
+// product.  Only if a lane's sum exceeds 2^8, or before the row's first key, the scores'
+// maximum is taken and everything rescaled.
+template <bool F8, int NB, int NH>
+__device__ __forceinline__ void ca_softmax(float* x, const CaScales<F8>* sc, float& m, float& l,
+                                           f32x4 (&o)[NB], bf16x8* pb) {
+  float p[4 * NH], sum = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 8 * PC; ++e) {
-    p[e] = exp2_fast(u[e] - m);
+  for (int e = 0; e < 4 * NH; ++e) {
+    p[e] = exp2_fast(x[e]);
     sum += p[e];
   }
-  if (__any(sum > kCaSum)) {
-    float mt = u[0];
+  if (__any(sum > kCaSum || m == kCaFloor)) {
+    float mt = x[0];
 #pragma unroll
-    for (int e = 1; e < 8 * PC; ++e) mt = fmaxf(mt, u[e]);
-    const float m_new = fmaxf(m, group_max(mt));
-    const float alpha = exp2_fast(m - m_new);
-    m = m_new;
+    for (int e = 1; e < 4 * NH; ++e) mt = fmaxf(mt, x[e]);
+    mt = group_max(mt);
+    const bool none = m == kCaFloor;
+    // a row that still sees nothing stays at the floor; its weights are zeros
+    const float shift = none ? (mt == -INFINITY ? 0.0f : mt) : fmaxf(mt, 0.0f);
+    const float alpha = none ? 0.0f : exp2_fast(-shift);
+    if (!none || mt != -INFINITY) m = ca_base(m) + shift;
     l *= alpha;
 #pragma unroll
     for (int db = 0; db < NB; ++db) o[db] *= alpha;
     sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8 * PC; ++e) {
-      p[e] = exp2_fast(u[e] - m_new);
+    for (int e = 0; e < 4 * NH; ++e) {
+      p[e] = exp2_fast(x[e] - shift);
       sum += p[e];
     }
   }
   l += sum;
 #pragma unroll
-  for (int e = 0; e < 8 * PC; ++e) {
+  for (int e = 0; e < 4 * NH; ++e) {
     if constexpr (F8) pb[e / 8][e % 8] = to_bf16(p[e] * sc[e / 4].v[e % 4]);
     else pb[e / 8][e % 8] = to_bf16(p[e]);
+  }
+}
+
+// The prefix values of a lane's four keys (c_off: of its head in a page) and the keys' scales,
+// of 16 keys that start at slot `slot` of page p.
+template <bool F8, int RT>
+__device__ __forceinline__ void ca_load_c(const CacheView& cv, int p, int hk, int slot,
+                                          const uint32_t (&c_off)[RT], int grp, f32x4* c,
+                                          uint32_t& ke, uint32_t& ve) {
+  const __amdgpu_buffer_rsrc_t rc = uniform_rsrc(
+      reinterpret_cast<const char*>(cv.c + cv.c_at(p, 0, 0)), (uint32_t)(cv.H << cv.page_shift) * 4);
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+    c[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, c_off[i], slot * 4, 0));
+  if constexpr (F8) {
+    const size_t row = cv.kv_row(p, hk, slot);
+    const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(reinterpret_cast<const char*>(cv.ke + row), 16);
+    const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(reinterpret_cast<const char*>(cv.ve + row), 16);
+    ke = __builtin_amdgcn_raw_buffer_load_b32(rk, 4 * grp, 0, 0);
+    ve = __builtin_amdgcn_raw_buffer_load_b32(rv, 4 * grp, 0, 0);
   }
 }
 
@@ -325,11 +361,13 @@ void attn_cache_kernel(
     }
   }
 
+  uint32_t c_off[RT];
   f32x4 oacc[RT][NB];
   float m[RT], l[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
-    m[i] = kCaFloor;
+    c_off[i] = (uint32_t)((head[i] << cv.page_shift) + 4 * grp) * 4;
+    m[i] = row_ok[i] ? kCaFloor : 0.0f;
     l[i] = 0.0f;
 #pragma unroll
     for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -366,14 +404,7 @@ void attn_cache_kernel(
       for (int i = 0; i < KL; ++i)
         t.h[hf].k[i] = __builtin_bit_cast(
             u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0, 0));
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-        t.h[hf].c[i] = *reinterpret_cast<const f32x4*>(
-            cv.c + cv.c_at(p, head[i], slot) + 4 * grp);
-      if constexpr (F8) {
-        t.h[hf].ke = *reinterpret_cast<const uint32_t*>(cv.ke + row + 4 * grp);
-        t.h[hf].ve = *reinterpret_cast<const uint32_t*>(cv.ve + row + 4 * grp);
-      }
+      ca_load_c<F8, RT>(cv, p, hk, slot, c_off, grp, t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
       // V: place s of the tile holds piece (s % CPR) ^ swizzle of key s / CPR
 #pragma unroll
       for (int i = 0; i < VL / 2; ++i) {
@@ -406,11 +437,12 @@ void attn_cache_kernel(
   // latency than the set did.
   Tile cur;
   const int first = k0 + wave * kCaTile;
+  const int last = first < k1 ? first + (k1 - 1 - first) / kCaRound * kCaRound : first - 1;
   int pg[2];
-  lookup(first, pg);
-  if (first < k1) issue(first, pg, cur);
-  lookup(first + kCaRound, pg);
-  for (int key0 = first; key0 < k1; key0 += kCaRound) {
+  lookup(last, pg);
+  if (first < k1) issue(last, pg, cur);
+  lookup(last - kCaRound, pg);
+  for (int key0 = last; key0 >= first; key0 -= kCaRound) {
     wait_all_memory();
     sched_fence();
     bf16x8 va[F8 ? 1 : NB];
@@ -443,27 +475,27 @@ void attn_cache_kernel(
     bf16x8 pb[RT];
     CaScales<F8> sc[2];
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-      sc[hf].set(cur.h[hf].ke, cur.h[hf].ve, scale_log2, plain ? 16 : cur.valid[hf] - 4 * grp);
-    float u[RT][8];
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-        ca_scores<F8>(u[i] + 4 * hf, s[i][hf], cur.h[hf].c[i], ci[i], sc[hf]);
+    for (int hf = 0; hf < 2; ++hf) sc[hf].set(cur.h[hf].ke, cur.h[hf].ve, scale_log2);
     if (!plain)
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int hf = 0; hf < 2; ++hf) sc[hf].clear_from(cur.valid[hf] - 4 * grp);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      float x[8];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+        ca_scores<F8>(x + 4 * hf, s[i][hf], cur.h[hf].c[i], ci[i], sc[hf], ca_base(m[i]));
+      if (!plain)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
-          ca_mask(u[i] + 4 * hf, row_ok[i] ? cur.valid[hf] - 4 * grp : 0,
+          ca_mask(x + 4 * hf, row_ok[i] ? cur.valid[hf] - 4 * grp : 0,
                   key0 + 16 * hf + 4 * grp - len, anc[i]);
-#pragma unroll
-    for (int i = 0; i < RT; ++i) ca_softmax<F8, NB, 1>(u[i], m[i], l[i], oacc[i], sc, &pb[i]);
+      ca_softmax<F8, NB, 2>(x, sc, m[i], l[i], oacc[i], &pb[i]);
+    }
     sched_fence();
     wait_lds();  // V is in registers
-    if (key0 + kCaRound < k1) issue(key0 + kCaRound, pg, cur);
-    lookup(key0 + 2 * kCaRound, pg);
+    if (key0 > first) issue(key0 - kCaRound, pg, cur);
+    lookup(key0 - 2 * kCaRound, pg);
     sched_fence();
 #pragma unroll
     for (int db = 0; db < NB; ++db) {
@@ -622,11 +654,13 @@ void attn_cache_rows_kernel(
     for (int s = 0; s < NS; ++s)
       qf[i][s] = *reinterpret_cast<const bf16x8*>(Q + out[i] * D + ca_dim<F8>(s, grp));
   }
+  uint32_t c_off[RT];
   f32x4 oacc[RT][NB];
   float m[RT], l[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
-    m[i] = kCaFloor;
+    c_off[i] = (uint32_t)((head[i] << cv.page_shift) + 4 * grp) * 4;
+    m[i] = row_ok[i] ? kCaFloor : 0.0f;
     l[i] = 0.0f;
 #pragma unroll
     for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -671,14 +705,7 @@ void attn_cache_rows_kernel(
       const bool there = cv.page_exists(pg[hf]) && key < T;
       const int p = __builtin_amdgcn_readfirstlane(there ? pg[hf] : 0);
       t.valid[hf] = there ? min(16, T - key) : 0;
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-        t.c[hf][i] = *reinterpret_cast<const f32x4*>(cv.c + cv.c_at(p, head[i], slot) + 4 * grp);
-      if constexpr (F8) {
-        const size_t row = cv.kv_row(p, hk, slot);
-        t.ke[hf] = *reinterpret_cast<const uint32_t*>(cv.ke + row + 4 * grp);
-        t.ve[hf] = *reinterpret_cast<const uint32_t*>(cv.ve + row + 4 * grp);
-      }
+      ca_load_c<F8, RT>(cv, p, hk, slot, c_off, grp, t.c[hf], t.ke[hf], t.ve[hf]);
     }
   };
 
@@ -731,27 +758,27 @@ void attn_cache_rows_kernel(
                        t.valid[2] == 16 && t.valid[3] == 16;
     CaScales<F8> sc[4];
 #pragma unroll
-    for (int hf = 0; hf < 4; ++hf)
-      sc[hf].set(t.ke[hf], t.ve[hf], scale_log2, plain ? 16 : t.valid[hf] - 4 * grp);
-    bf16x8 pb[RT][2];
-    float u[RT][16];
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int hf = 0; hf < 4; ++hf)
-        ca_scores<F8>(u[i] + 4 * hf, s[i][hf], t.c[hf][i], ci[i], sc[hf]);
+    for (int hf = 0; hf < 4; ++hf) sc[hf].set(t.ke[hf], t.ve[hf], scale_log2);
     if (!plain)
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int hf = 0; hf < 4; ++hf) sc[hf].clear_from(t.valid[hf] - 4 * grp);
+    bf16x8 pb[RT][2];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      float x[16];
+#pragma unroll
+      for (int hf = 0; hf < 4; ++hf)
+        ca_scores<F8>(x + 4 * hf, s[i][hf], t.c[hf][i], ci[i], sc[hf], ca_base(m[i]));
+      if (!plain)
 #pragma unroll
         for (int hf = 0; hf < 4; ++hf)
-          ca_mask(u[i] + 4 * hf, row_ok[i] ? t.valid[hf] - 4 * grp : 0,
+          ca_mask(x + 4 * hf, row_ok[i] ? t.valid[hf] - 4 * grp : 0,
                   key0 + 16 * hf + 4 * grp - len, anc[i]);
-#pragma unroll
-    for (int i = 0; i < RT; ++i) ca_softmax<F8, NB, 2>(u[i], m[i], l[i], oacc[i], sc, pb[i]);
+      ca_softmax<F8, NB, 4>(x, sc, m[i], l[i], oacc[i], pb[i]);
+    }
     sched_fence();
-    if (key0 + kCrTile < k1) issue_c(key0 + kCrTile, pg, t);
-    lookup(key0 + 2 * kCrTile, pg);
+    if (key0 > k0) issue_c(key0 - kCrTile, pg, t);
+    lookup(key0 - 2 * kCrTile, pg);
     sched_fence();
     static_for<2>([&](auto pc) {
       constexpr int P = decltype(pc)::value;  // 32 keys
@@ -784,26 +811,25 @@ void attn_cache_rows_kernel(
     });
   };
 
-  lookup(k0, pg);
-  int own = cv.page_entry(b, k0 + 16 * wave);
-  if (k0 < k1) {
-    issue_kv(k0, own, std::integral_constant<int, 0>());
-    issue_c(k0, pg, t);
-  }
-  lookup(k0 + kCrTile, pg);
-  own = cv.page_entry(b, k0 + kCrTile + 16 * wave);
+  const int last = k0 + (k1 - 1 - k0) / kCrTile * kCrTile;  // (a piece has a key)
+  lookup(last, pg);
+  int own = cv.page_entry(b, last + 16 * wave);
+  issue_kv(last, own, std::integral_constant<int, 0>());
+  issue_c(last, pg, t);
+  lookup(last - kCrTile, pg);
+  own = cv.page_entry(b, last - kCrTile + 16 * wave);
   auto step = [&](int key0, auto bufc) {
     constexpr int B = decltype(bufc)::value;
     wait_all_memory();
     __syncthreads();  // the tile is in LDS and everybody is done with the one before it
-    if (key0 + kCrTile < k1) issue_kv(key0 + kCrTile, own, std::integral_constant<int, 1 - B>());
-    own = cv.page_entry(b, key0 + 2 * kCrTile + 16 * wave);
+    if (key0 > k0) issue_kv(key0 - kCrTile, own, std::integral_constant<int, 1 - B>());
+    own = cv.page_entry(b, key0 - 2 * kCrTile + 16 * wave);
     sched_fence();
     body(key0, bufc);
   };
-  for (int key0 = k0; key0 < k1; key0 += 2 * kCrTile) {
+  for (int key0 = last; key0 >= k0; key0 -= 2 * kCrTile) {
     step(key0, std::integral_constant<int, 0>());
-    if (key0 + kCrTile < k1) step(key0 + kCrTile, std::integral_constant<int, 1>());
+    if (key0 > k0) step(key0 - kCrTile, std::integral_constant<int, 1>());
   }
 
 #pragma unroll

@@ -26,11 +26,11 @@ struct CacheView {
     const int p = table[(size_t)b * max_pages + i];
     return (unsigned)p < (unsigned)n_pages ? p : -1;
   }
-  // The table's entry for position pos (of the table's last place, past its end), unchecked,
-  // by a scalar load: pos is the same in the whole wave.  page_exists() says whether it is one.
+  // The table's entry for position pos (outside the table, of its nearest place), unchecked, by
+  // a scalar load: pos is the same in the whole wave.  page_exists() says whether it is a page.
   __device__ int page_entry(int b, int pos) const {
     typedef const __attribute__((address_space(4))) int table_t;
-    const int i = min(pos >> page_shift, max_pages - 1);
+    const int i = min(max(pos, 0) >> page_shift, max_pages - 1);
     return ((table_t*)(uintptr_t)table)[(size_t)b * max_pages + i];
   }
   __device__ bool page_exists(int p) const { return (unsigned)p < (unsigned)n_pages; }
