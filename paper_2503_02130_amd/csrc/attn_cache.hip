@@ -80,12 +80,10 @@ __device__ __forceinline__ int v_swizzle(int key) {
   }
 }
 
-// The ancestors of new token `lane` and itself, as bits (pointers doubled).
-__device__ __forceinline__ uint64_t ancestors(const int* __restrict__ parent, int nn, int lane) {
+// The ancestors of new token `lane`, whose parent is `up`, and itself, as bits (pointers doubled).
+__device__ __forceinline__ uint64_t ancestors(int up, int nn, int lane) {
   uint64_t bits = 1ull << lane;
-  int up = -1;
-  if (lane < nn) up = parent ? parent[lane] : lane - 1;
-  if (up >= lane) up = -1;
+  if (lane >= nn || up >= lane) up = -1;
   while (__any(up >= 0)) {
     const int from = up >= 0 ? up : lane;
     const uint32_t lo = __shfl((uint32_t)bits, from), hi = __shfl((uint32_t)(bits >> 32), from);
@@ -116,15 +114,17 @@ __device__ __forceinline__ bool ca_piece(const CacheView& cv, const int* __restr
                                          const int* __restrict__ n_new, int n, const CaSplit& sp,
                                          int piece, int lane, CaPiece& out) {
   const int cap = (int)cv.capacity();
+  int len = 0, nn = 0;  // of the lane's sequence
   auto units_of = [&](int b) {
-    if (b >= cv.B) return 0;
-    const int nn = n_new ? max(0, min(n_new[b], n)) : n;
-    const int T = min(min(max(seq_len[b], 0), cap) + nn, cap);
-    return nn == 0 ? 0 : (T + sp.unit - 1) / sp.unit;
+    const int at = min(b, cv.B - 1);
+    len = min(max(seq_len[at], 0), cap);
+    nn = n_new ? max(0, min(n_new[at], n)) : n;
+    return b >= cv.B || nn == 0 ? 0 : (min(len + nn, cap) + sp.unit - 1) / sp.unit;
   };
+  const int u0 = units_of(lane);
   long long total = 0;
   for (int b0 = 0; b0 < cv.B; b0 += 64) {
-    long long u = units_of(b0 + lane);
+    long long u = b0 == 0 ? u0 : units_of(b0 + lane);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) u += __shfl_xor(u, off);
     total += u;
@@ -133,7 +133,7 @@ __device__ __forceinline__ bool ca_piece(const CacheView& cv, const int* __restr
                                   : (int)max((long long)sp.min_units, (total + sp.target - 1) / sp.target);
   int first = 0;
   for (int b0 = 0; b0 < cv.B; b0 += 64) {
-    const int u = units_of(b0 + lane), pieces = u / most + (u % most != 0);
+    const int u = cv.B <= 64 ? u0 : units_of(b0 + lane), pieces = u / most + (u % most != 0);
     int incl = pieces;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -143,14 +143,13 @@ __device__ __forceinline__ bool ca_piece(const CacheView& cv, const int* __restr
     const uint64_t past = __ballot(first + incl > piece);
     if (past) {
       const int l = __builtin_ctzll(past);
-      const int b = b0 + l;
-      out.b = b;
+      out.b = b0 + l;
       out.count = __builtin_amdgcn_readlane(pieces, l);
       out.first = first + __builtin_amdgcn_readlane(incl, l) - out.count;
       out.split = piece - out.first;
-      out.len = min(max(seq_len[b], 0), cap);
-      out.nn = n_new ? max(0, min(n_new[b], n)) : n;
-      out.T = __builtin_amdgcn_readfirstlane(min(out.len + out.nn, cap));
+      out.len = __builtin_amdgcn_readlane(len, l);
+      out.nn = __builtin_amdgcn_readlane(nn, l);
+      out.T = min(out.len + out.nn, cap);
       const int units = __builtin_amdgcn_readlane(u, l);
       const int per = (units + out.count - 1) / out.count * sp.unit;
       out.k0 = out.split * per;
@@ -291,6 +290,65 @@ __device__ __forceinline__ void ca_load_c(const CacheView& cv, int p, int hk, in
   }
 }
 
+// A lane's rows, one of each row tile of its wave: row r is token r % n of head r / n of the
+// key head's group.
+template <int D, bool F8, int RT>
+struct CaRows {
+  int head[RT], tok[RT];
+  bool mine[RT];    // a row of this call
+  bool ok[RT];      // whose own place is in the cache; any other has no c and sees nothing
+  float ci[RT];
+  uint64_t anc[RT];
+  uint32_t c_off[RT];
+  bf16x8 q[RT][D / 32];
+
+  __device__ __forceinline__ void place(const CacheView& cv, const CaPiece& pc, int row0, int hk,
+                                        int G, int n, int grp) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int r = row0 + 16 * i, g = r / n;
+      tok[i] = r - g * n;
+      mine[i] = g < G && tok[i] < pc.nn;
+      head[i] = hk * G + (mine[i] ? g : 0);
+      tok[i] = mine[i] ? tok[i] : 0;
+      c_off[i] = (uint32_t)((head[i] << cv.page_shift) + 4 * grp) * 4;
+    }
+  }
+  // row of O and LSE
+  __device__ __forceinline__ size_t out(int i, int b, int H, int n) const {
+    return ((size_t)b * H + head[i]) * n + tok[i];
+  }
+  // Every load is issued whether its lane needs it or not, so that they wait for each other
+  // once and not one by one.
+  __device__ __forceinline__ void load(const CacheView& cv, const CaPiece& pc,
+                                       const bf16* __restrict__ Q, const int* __restrict__ parent,
+                                       int n, int lane, int grp) {
+    int up = lane - 1, own[RT];
+    if (parent) up = parent[(size_t)pc.b * n + min(lane, n - 1)];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+      own[i] = cv.table[(size_t)pc.b * cv.max_pages +
+                        min((pc.len + tok[i]) >> cv.page_shift, cv.max_pages - 1)];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s)
+        q[i][s] = *reinterpret_cast<const bf16x8*>(Q + out(i, pc.b, cv.H, n) * D + ca_dim<F8>(s, grp));
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      ok[i] = mine[i] && pc.len + tok[i] < (int)cv.capacity() && cv.page_exists(own[i]);
+      ci[i] = cv.c[cv.c_at(ok[i] ? own[i] : 0, head[i], cv.slot_of(pc.len + tok[i]))];
+    }
+    const uint64_t bits = pc.k1 > pc.len ? ancestors(up, pc.nn, lane) : 0;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const uint32_t lo = __shfl((uint32_t)bits, tok[i]), hi = __shfl((uint32_t)(bits >> 32), tok[i]);
+      anc[i] = ((uint64_t)hi << 32) | lo;
+      ci[i] = ok[i] ? ci[i] : -INFINITY;
+    }
+  }
+};
+
 template <int D, int RT>
 struct CaMerge {
   float o[kCaWaves][16][D + 4];  // one row tile at a time
@@ -334,45 +392,8 @@ void attn_cache_kernel(
     parts.table[b] = make_int2(pc.first, pc.count);
   const int col = lane & 15, grp = lane >> 4;
 
-  // this lane's rows
-  int head[RT], tok[RT];
-  bool row_ok[RT];       // a row of this call
-  float ci[RT];
-  uint64_t anc[RT];
-  bf16x8 qf[RT][NS];
-  const uint64_t bits = k1 > len ? ancestors(parent ? parent + (size_t)b * n : nullptr, nn, lane) : 0;
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int r = (rb * RT + i) * 16 + col;
-    const int g = r / n;
-    tok[i] = r - g * n;
-    row_ok[i] = g < G && tok[i] < nn;
-    head[i] = hk * G + (row_ok[i] ? g : 0);
-    // a token whose own place is not in the cache has no c and sees nothing
-    const int own = row_ok[i] && len + tok[i] < cap ? cv.page_of(b, len + tok[i]) : -1;
-    ci[i] = own < 0 ? -INFINITY : cv.c[cv.c_at(own, head[i], cv.slot_of(len + tok[i]))];
-    const uint32_t lo = __shfl((uint32_t)bits, tok[i]), hi = __shfl((uint32_t)(bits >> 32), tok[i]);
-    anc[i] = ((uint64_t)hi << 32) | lo;
-    if (own < 0) row_ok[i] = false;
-    const bf16* q = Q + (((size_t)b * cv.H + head[i]) * n + (row_ok[i] ? tok[i] : 0)) * D;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      qf[i][s] = *reinterpret_cast<const bf16x8*>(q + ca_dim<F8>(s, grp));
-    }
-  }
-
-  uint32_t c_off[RT];
-  f32x4 oacc[RT][NB];
-  float m[RT], l[RT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    c_off[i] = (uint32_t)((head[i] << cv.page_shift) + 4 * grp) * 4;
-    m[i] = row_ok[i] ? kCaFloor : 0.0f;
-    l[i] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
+  CaRows<D, F8, RT> rows;
+  rows.place(cv, pc, rb * RT * 16 + col, hk, G, n, grp);
   struct Half {       // 16 keys of one page
     u32x4d k[KL];
     f32x4 c[RT];
@@ -404,7 +425,7 @@ void attn_cache_kernel(
       for (int i = 0; i < KL; ++i)
         t.h[hf].k[i] = __builtin_bit_cast(
             u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0, 0));
-      ca_load_c<F8, RT>(cv, p, hk, slot, c_off, grp, t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
+      ca_load_c<F8, RT>(cv, p, hk, slot, rows.c_off, grp, t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
       // V: place s of the tile holds piece (s % CPR) ^ swizzle of key s / CPR
 #pragma unroll
       for (int i = 0; i < VL / 2; ++i) {
@@ -442,6 +463,16 @@ void attn_cache_kernel(
   lookup(last, pg);
   if (first < k1) issue(last, pg, cur);
   lookup(last - kCaRound, pg);
+  rows.load(cv, pc, Q, parent, n, lane, grp);
+  f32x4 oacc[RT][NB];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    m[i] = rows.ok[i] ? kCaFloor : 0.0f;
+    l[i] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   for (int key0 = last; key0 >= first; key0 -= kCaRound) {
     wait_all_memory();
     sched_fence();
@@ -468,7 +499,7 @@ void attn_cache_kernel(
       for (int st = 0; st < NS; ++st) {
         const bf16x8 ka = k_operand<F8>(cur.h[hf].k, st);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, qf[i][st], s[i][hf]);
+        for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, rows.q[i][st], s[i][hf]);
       }
     }
     const bool plain = cur.valid[0] == 16 && cur.valid[1] == 16 && key0 + kCaTile <= len;
@@ -484,12 +515,12 @@ void attn_cache_kernel(
       float x[8];
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
-        ca_scores<F8>(x + 4 * hf, s[i][hf], cur.h[hf].c[i], ci[i], sc[hf], ca_base(m[i]));
+        ca_scores<F8>(x + 4 * hf, s[i][hf], cur.h[hf].c[i], rows.ci[i], sc[hf], ca_base(m[i]));
       if (!plain)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
-          ca_mask(x + 4 * hf, row_ok[i] ? cur.valid[hf] - 4 * grp : 0,
-                  key0 + 16 * hf + 4 * grp - len, anc[i]);
+          ca_mask(x + 4 * hf, rows.ok[i] ? cur.valid[hf] - 4 * grp : 0,
+                  key0 + 16 * hf + 4 * grp - len, rows.anc[i]);
       ca_softmax<F8, NB, 2>(x, sc, m[i], l[i], oacc[i], &pb[i]);
     }
     sched_fence();
@@ -630,42 +661,8 @@ void attn_cache_rows_kernel(
     parts.table[b] = make_int2(pc.first, pc.count);
   const int col = lane & 15, grp = lane >> 4;
 
-  int head[RT];
-  bool row_ok[RT];
-  float ci[RT];
-  uint64_t anc[RT];
-  size_t out[RT];  // the row in O and LSE; of a row that is not there, unused
-  bool mine[RT];
-  bf16x8 qf[RT][NS];
-  const uint64_t bits = k1 > len ? ancestors(parent ? parent + (size_t)b * n : nullptr, nn, lane) : 0;
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int r = ((rb * kCaWaves + wave) * RT + i) * 16 + col;
-    const int g = r / n, tok = r - g * n;
-    mine[i] = g < G && tok < nn;
-    head[i] = hk * G + (mine[i] ? g : 0);
-    const int own = mine[i] && len + tok < cap ? cv.page_of(b, len + tok) : -1;
-    row_ok[i] = own >= 0;
-    ci[i] = own < 0 ? -INFINITY : cv.c[cv.c_at(own, head[i], cv.slot_of(len + tok))];
-    const uint32_t lo = __shfl((uint32_t)bits, tok), hi = __shfl((uint32_t)(bits >> 32), tok);
-    anc[i] = ((uint64_t)hi << 32) | lo;
-    out[i] = ((size_t)b * cv.H + head[i]) * n + (mine[i] ? tok : 0);
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
-      qf[i][s] = *reinterpret_cast<const bf16x8*>(Q + out[i] * D + ca_dim<F8>(s, grp));
-  }
-  uint32_t c_off[RT];
-  f32x4 oacc[RT][NB];
-  float m[RT], l[RT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    c_off[i] = (uint32_t)((head[i] << cv.page_shift) + 4 * grp) * 4;
-    m[i] = row_ok[i] ? kCaFloor : 0.0f;
-    l[i] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
+  CaRows<D, F8, RT> rows;
+  rows.place(cv, pc, (rb * kCaWaves + wave) * RT * 16 + col, hk, G, n, grp);
   // K and V of a tile to LDS: a wave moves its own 16 keys.  The lane's source offsets are
   // formed anew for each tile (a few operations; kept, they would be spilled).
   auto issue_kv = [&](int key0, int entry, auto bufc) {
@@ -705,7 +702,7 @@ void attn_cache_rows_kernel(
       const bool there = cv.page_exists(pg[hf]) && key < T;
       const int p = __builtin_amdgcn_readfirstlane(there ? pg[hf] : 0);
       t.valid[hf] = there ? min(16, T - key) : 0;
-      ca_load_c<F8, RT>(cv, p, hk, slot, c_off, grp, t.c[hf], t.ke[hf], t.ve[hf]);
+      ca_load_c<F8, RT>(cv, p, hk, slot, rows.c_off, grp, t.c[hf], t.ke[hf], t.ve[hf]);
     }
   };
 
@@ -736,6 +733,23 @@ void attn_cache_rows_kernel(
 
   Tile t;
   int pg[4];  // the next tile's pages
+  const int last = k0 + (k1 - 1 - k0) / kCrTile * kCrTile;  // (a piece has a key)
+  lookup(last, pg);
+  int own = cv.page_entry(b, last + 16 * wave);
+  issue_kv(last, own, std::integral_constant<int, 0>());
+  issue_c(last, pg, t);
+  lookup(last - kCrTile, pg);
+  own = cv.page_entry(b, last - kCrTile + 16 * wave);
+  rows.load(cv, pc, Q, parent, n, lane, grp);
+  f32x4 oacc[RT][NB];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    m[i] = rows.ok[i] ? kCaFloor : 0.0f;
+    l[i] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   auto body = [&](int key0, auto bufc) {
     constexpr int B = decltype(bufc)::value;
     f32x4 s[RT][4];
@@ -751,7 +765,7 @@ void attn_cache_rows_kernel(
       for (int st = 0; st < NS; ++st) {
         const bf16x8 ka = k_operand<F8>(kw, st);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, qf[i][st], s[i][hf]);
+        for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, rows.q[i][st], s[i][hf]);
       }
     }
     const bool plain = key0 + kCrTile <= len && t.valid[0] == 16 && t.valid[1] == 16 &&
@@ -768,12 +782,12 @@ void attn_cache_rows_kernel(
       float x[16];
 #pragma unroll
       for (int hf = 0; hf < 4; ++hf)
-        ca_scores<F8>(x + 4 * hf, s[i][hf], t.c[hf][i], ci[i], sc[hf], ca_base(m[i]));
+        ca_scores<F8>(x + 4 * hf, s[i][hf], t.c[hf][i], rows.ci[i], sc[hf], ca_base(m[i]));
       if (!plain)
 #pragma unroll
         for (int hf = 0; hf < 4; ++hf)
-          ca_mask(x + 4 * hf, row_ok[i] ? t.valid[hf] - 4 * grp : 0,
-                  key0 + 16 * hf + 4 * grp - len, anc[i]);
+          ca_mask(x + 4 * hf, rows.ok[i] ? t.valid[hf] - 4 * grp : 0,
+                  key0 + 16 * hf + 4 * grp - len, rows.anc[i]);
       ca_softmax<F8, NB, 4>(x, sc, m[i], l[i], oacc[i], pb[i]);
     }
     sched_fence();
@@ -811,13 +825,6 @@ void attn_cache_rows_kernel(
     });
   };
 
-  const int last = k0 + (k1 - 1 - k0) / kCrTile * kCrTile;  // (a piece has a key)
-  lookup(last, pg);
-  int own = cv.page_entry(b, last + 16 * wave);
-  issue_kv(last, own, std::integral_constant<int, 0>());
-  issue_c(last, pg, t);
-  lookup(last - kCrTile, pg);
-  own = cv.page_entry(b, last - kCrTile + 16 * wave);
   auto step = [&](int key0, auto bufc) {
     constexpr int B = decltype(bufc)::value;
     wait_all_memory();
@@ -835,7 +842,8 @@ void attn_cache_rows_kernel(
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     const float lt = group_sum(l[i]);
-    if (!mine[i]) continue;
+    if (!rows.mine[i]) continue;
+    const size_t R = rows.out(i, b, cv.H, n);
     if (pc.count == 1) {
       const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;  // a row without a key: zeros, -inf
 #pragma unroll
@@ -843,12 +851,12 @@ void attn_cache_rows_kernel(
         bf16x4 w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = to_bf16(oacc[i][db][j] * inv);
-        *reinterpret_cast<bf16x4*>(O + out[i] * D + 16 * db + 4 * grp) = w;
+        *reinterpret_cast<bf16x4*>(O + R * D + 16 * db + 4 * grp) = w;
       }
-      if (grp == 0) LSE[out[i]] = lt > 0.0f ? kLn2 * (m[i] + log2f(lt)) : -INFINITY;
+      if (grp == 0) LSE[R] = lt > 0.0f ? kLn2 * (m[i] + log2f(lt)) : -INFINITY;
     } else {
-      // (piece, head, token): out[i] without its sequence
-      const size_t at = (size_t)(pc.first + pc.split - b) * cv.H * n + out[i];
+      // (piece, head, token): R without its sequence
+      const size_t at = (size_t)(pc.first + pc.split - b) * cv.H * n + R;
 #pragma unroll
       for (int db = 0; db < NB; ++db)
         *reinterpret_cast<f32x4*>(parts.o + at * D + 16 * db + 4 * grp) = oacc[i][db];
