@@ -628,7 +628,7 @@ typedef struct {
  *     index [B,n] int32 in;  n_keep [B] int32 in
  * fox_cache_read: positions start[b] + t, t < T, below seq_len[b], as dtype: k, v
  *   [B,H_kv,T,d], c [B,H,T] fp32 (may be NULL); start may be NULL (0).  Other rows of the
- *   outputs are left as they were.
+ *   outputs are left as they were, or set to zero if zero_others is not 0.
  */
 fox_status_t fox_cache_append(const fox_cache_t* cache, fox_dtype_t dtype, const void* k, const void* v,
                      const float* gate_logit, const int* seq_len, const int* parent,
@@ -639,7 +639,8 @@ fox_status_t fox_cache_append_packed(const fox_cache_t* cache, fox_dtype_t dtype
 fox_status_t fox_cache_keep(const fox_cache_t* cache, const int* seq_len, const int* index,
                    const int* n_keep, int n, hipStream_t stream);
 fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const int* start,
-                   const int* seq_len, void* k, void* v, float* c, int T, hipStream_t stream);
+                   const int* seq_len, void* k, void* v, float* c, int T, int zero_others,
+                   hipStream_t stream);
 
 /*
  * Attention of n new tokens of each sequence (1 <= n <= 64) over the cache that holds them

@@ -7,8 +7,8 @@ from typing import Optional, Tuple
 
 import torch
 
-from ._lib import (_DT, _check, _on_device, _ptr, _raise, _raw_stream, _workspace, default_scale,
-                   load)
+from ._lib import (_DT, _call, _check, _need, _ptr, _raise, _workspace, _workspace_bytes,
+                   default_scale, load)
 
 FOX_CACHE_BF16 = 0
 FOX_CACHE_E4M3 = 1
@@ -76,7 +76,7 @@ class PagedCache:
 
 def _check_lens(t: Optional[torch.Tensor], name: str, B: int, device):
     if t is not None:
-        _check(t, name, (B,), torch.int32, device)
+        _need(t, name, (B,), torch.int32, device)
 
 
 def fox_cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
@@ -89,17 +89,15 @@ def fox_cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
     n, dt, dev = k.shape[2], k.dtype, cache.device
     if dt not in _DT:
         raise ValueError(f"unsupported dtype {dt}")
-    _check(k, "k", (cache.B, cache.H_kv, n, cache.d), dt, dev)
-    _check(v, "v", (cache.B, cache.H_kv, n, cache.d), dt, dev)
-    _check(gate_logit, "gate_logit", (cache.B, cache.H, n), torch.float32, dev)
-    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    _need(k, "k", (cache.B, cache.H_kv, n, cache.d), dt, dev)
+    _need(v, "v", (cache.B, cache.H_kv, n, cache.d), dt, dev)
+    _need(gate_logit, "gate_logit", (cache.B, cache.H, n), torch.float32, dev)
+    _need(seq_len, "seq_len", (cache.B,), torch.int32, dev)
     if parent is not None:
-        _check(parent, "parent", (cache.B, n), torch.int32, dev)
+        _need(parent, "parent", (cache.B, n), torch.int32, dev)
     _check_lens(n_new, "n_new", cache.B, dev)
-    with _on_device(dev):
-        st = load().fox_cache_append(cache._ref, _DT[dt], _ptr(k), _ptr(v), _ptr(gate_logit),
-                                     _ptr(seq_len), _ptr(parent), _ptr(n_new), n,
-                                     _raw_stream(dev.index))
+    st = _call(load().fox_cache_append, dev, cache._ref, _DT[dt], _ptr(k), _ptr(v),
+               _ptr(gate_logit), _ptr(seq_len), _ptr(parent), _ptr(n_new), n)
     _raise(st, "fox_cache_append")
 
 
@@ -112,15 +110,13 @@ def fox_cache_append_packed(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
     N, dt, dev = k.shape[1], k.dtype, cache.device
     if dt not in _DT:
         raise ValueError(f"unsupported dtype {dt}")
-    _check(k, "k", (cache.H_kv, N, cache.d), dt, dev)
-    _check(v, "v", (cache.H_kv, N, cache.d), dt, dev)
-    _check(c, "c", (cache.H, N), torch.float32, dev)
-    _check(cu_seqlens, "cu_seqlens", (cache.B + 1,), torch.int32, dev)
+    _need(k, "k", (cache.H_kv, N, cache.d), dt, dev)
+    _need(v, "v", (cache.H_kv, N, cache.d), dt, dev)
+    _need(c, "c", (cache.H, N), torch.float32, dev)
+    _need(cu_seqlens, "cu_seqlens", (cache.B + 1,), torch.int32, dev)
     _check_lens(seq_len, "seq_len", cache.B, dev)
-    with _on_device(dev):
-        st = load().fox_cache_append_packed(cache._ref, _DT[dt], _ptr(k), _ptr(v), _ptr(c),
-                                            _ptr(cu_seqlens), _ptr(seq_len), N,
-                                            _raw_stream(dev.index))
+    st = _call(load().fox_cache_append_packed, dev, cache._ref, _DT[dt], _ptr(k), _ptr(v),
+               _ptr(c), _ptr(cu_seqlens), _ptr(seq_len), N)
     _raise(st, "fox_cache_append_packed")
 
 
@@ -130,12 +126,11 @@ def fox_cache_keep(cache: PagedCache, seq_len: torch.Tensor, index: torch.Tensor
     accepted path of a tree of drafts.  index [B,n] (n <= 64), n_keep [B] int32.  seq_len is
     left to the caller, who adds n_keep to it."""
     n, dev = index.shape[1], cache.device
-    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
-    _check(index, "index", (cache.B, n), torch.int32, dev)
-    _check(n_keep, "n_keep", (cache.B,), torch.int32, dev)
-    with _on_device(dev):
-        st = load().fox_cache_keep(cache._ref, _ptr(seq_len), _ptr(index), _ptr(n_keep), n,
-                                   _raw_stream(dev.index))
+    _need(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    _need(index, "index", (cache.B, n), torch.int32, dev)
+    _need(n_keep, "n_keep", (cache.B,), torch.int32, dev)
+    st = _call(load().fox_cache_keep, dev, cache._ref, _ptr(seq_len), _ptr(index), _ptr(n_keep),
+               n)
     _raise(st, "fox_cache_keep")
 
 
@@ -145,24 +140,29 @@ def fox_cache_read(cache: PagedCache, seq_len: torch.Tensor, T: int,
                    c: Optional[torch.Tensor] = None
                    ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Positions start[b] + t, t < T, below seq_len[b], as (k, v [B,H_kv,T,d], c [B,H,T]
-    fp32).  Rows without a token keep what k, v, c held (given: theirs; else zeros)."""
+    fp32).  Given k, v and c are filled; their rows without a token are left as they were.
+    Otherwise such rows are zero."""
     dev = cache.device
     if k is not None:
         dtype = k.dtype
     if dtype not in _DT:
         raise ValueError(f"unsupported dtype {dtype}")
     shape = (cache.B, cache.H_kv, T, cache.d)
-    k = torch.zeros(shape, device=dev, dtype=dtype) if k is None else k
-    v = torch.zeros(shape, device=dev, dtype=dtype) if v is None else v
-    c = torch.zeros((cache.B, cache.H, T), device=dev) if c is None else c
-    _check(k, "k", shape, dtype, dev)
-    _check(v, "v", shape, dtype, dev)
-    _check(c, "c", (cache.B, cache.H, T), torch.float32, dev)
-    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    given = [x is not None for x in (k, v, c)]
+    if any(given) and not all(given):
+        raise ValueError("k, v and c are given together or not at all")
+    if k is None:
+        k = torch.empty(shape, device=dev, dtype=dtype)
+        v = torch.empty(shape, device=dev, dtype=dtype)
+        c = torch.empty((cache.B, cache.H, T), device=dev, dtype=torch.float32)
+    else:
+        _need(k, "k", shape, dtype, dev)
+        _need(v, "v", shape, dtype, dev)
+        _need(c, "c", (cache.B, cache.H, T), torch.float32, dev)
+    _need(seq_len, "seq_len", (cache.B,), torch.int32, dev)
     _check_lens(start, "start", cache.B, dev)
-    with _on_device(dev):
-        st = load().fox_cache_read(cache._ref, _DT[dtype], _ptr(start), _ptr(seq_len), _ptr(k),
-                                   _ptr(v), _ptr(c), T, _raw_stream(dev.index))
+    st = _call(load().fox_cache_read, dev, cache._ref, _DT[dtype], _ptr(start), _ptr(seq_len),
+               _ptr(k), _ptr(v), _ptr(c), T, not given[0])
     _raise(st, "fox_cache_read")
     return k, v, c
 
@@ -183,10 +183,10 @@ def fox_attn_cache(q: torch.Tensor, cache: PagedCache, seq_len: torch.Tensor,
     ones included (0: what the page table holds); it sets how the keys are split."""
     B, H, n, d = q.shape
     dev = cache.device
-    _check(q, "q", (cache.B, cache.H, n, cache.d), torch.bfloat16, dev)
-    _check(seq_len, "seq_len", (cache.B,), torch.int32, dev)
+    _need(q, "q", (cache.B, cache.H, n, cache.d), torch.bfloat16, dev)
+    _need(seq_len, "seq_len", (cache.B,), torch.int32, dev)
     if parent is not None:
-        _check(parent, "parent", (B, n), torch.int32, dev)
+        _need(parent, "parent", (B, n), torch.int32, dev)
     _check_lens(n_new, "n_new", B, dev)
     if n_new is not None and (o is None or lse is None):
         # rows that a sequence does not have are not written
@@ -195,22 +195,20 @@ def fox_attn_cache(q: torch.Tensor, cache: PagedCache, seq_len: torch.Tensor,
     if o is None:
         o = torch.empty_like(q)
     else:
-        _check(o, "o", (B, H, n, d), torch.bfloat16, dev)
+        _need(o, "o", (B, H, n, d), torch.bfloat16, dev)
     if lse is None:
         lse = torch.empty((B, H, n), device=dev, dtype=torch.float32)
     else:
-        _check(lse, "lse", (B, H, n), torch.float32, dev)
+        _need(lse, "lse", (B, H, n), torch.float32, dev)
     lib = load()
     if workspace is None:
         nbytes = lib.fox_attn_cache_workspace_bytes(cache._ref, n, max_len)
         if nbytes:
             workspace = _workspace(nbytes, dev)
     else:
-        nbytes = workspace.numel() * workspace.element_size()
+        nbytes = _workspace_bytes(workspace, dev)
     s = default_scale(d) if scale is None else float(scale)
-    with _on_device(dev):
-        st = lib.fox_attn_cache(cache._ref, _ptr(q), _ptr(seq_len), _ptr(parent), _ptr(n_new),
-                                _ptr(o), _ptr(lse), _ptr(workspace), nbytes, n, max_len, s,
-                                _raw_stream(dev.index))
+    st = _call(lib.fox_attn_cache, dev, cache._ref, _ptr(q), _ptr(seq_len), _ptr(parent),
+               _ptr(n_new), _ptr(o), _ptr(lse), _ptr(workspace), nbytes, n, max_len, s)
     _raise(st, "fox_attn_cache")
     return o, lse

@@ -173,7 +173,7 @@ def load() -> ctypes.CDLL:
             ("fox_cache_append", [P, I, P, P, P, P, P, P, I, P]),
             ("fox_cache_append_packed", [P, I, P, P, P, P, P, I, P]),
             ("fox_cache_keep", [P, P, P, P, I, P]),
-            ("fox_cache_read", [P, I, P, P, P, P, P, I, P]),
+            ("fox_cache_read", [P, I, P, P, P, P, P, I, I, P]),
             ("fox_attn_cache", [P, P, P, P, P, P, P, P, Z, I, I, F, P]),
             ("fox_packed_plan", [P, I, I, P, Z, P]),
             ("fox_gate_prefix_packed", [I, P, P, P, I, I, I, P]),
@@ -215,21 +215,20 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-class _NoGuard:
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        return False
-
-
-_NO_GUARD = _NoGuard()
+def _call(entry, device, *args) -> int:
+    """entry(*args, stream) with `device` the current one (a kernel is launched on a stream of
+    the current device), on its current stream."""
+    if device.index == _get_device():
+        return entry(*args, _raw_stream(device.index))
+    with torch.cuda.device(device):
+        return entry(*args, _raw_stream(device.index))
 
 
-def _on_device(device):
-    """A context in which `device` is the current one (a kernel is launched on a stream of the
-    current device); nothing where it is already."""
-    return _NO_GUARD if device.index == _get_device() else torch.cuda.device(device)
+def _need(t, name: str, shape, dtype, device):
+    """_check's decision for a tensor on a known device, in fewer steps."""
+    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype
+            and t.get_device() == device.index and t.is_contiguous()):
+        _check(t, name, shape, dtype, device)
 
 
 def _check(t: torch.Tensor, name: str, shape, dtype, device):
@@ -255,6 +254,13 @@ def _check(t: torch.Tensor, name: str, shape, dtype, device):
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(nbytes, 16), device=device, dtype=torch.uint8)
+
+
+def _workspace_bytes(t: torch.Tensor, device) -> int:
+    """The size of a workspace that the caller brought."""
+    if t.get_device() != device.index or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    return t.numel() * t.element_size()
 
 
 def _raise(status: int, what: str):

@@ -7,8 +7,8 @@ from typing import Optional, Sequence, Tuple
 
 import torch
 
-from ._lib import (_DT, _check, _on_device, _ptr, _raise, _raw_stream, _workspace, default_scale,
-                   load)
+from ._lib import (_DT, _call, _check, _need, _ptr, _raise, _workspace, _workspace_bytes,
+                   default_scale, load)
 
 
 class _RowsStruct(ctypes.Structure):
@@ -24,8 +24,13 @@ def _check_cu(cu: torch.Tensor, device):
     return B
 
 
+def _plan_places(B: int, N: int) -> int:
+    """Places of fox_packed_plan_bytes(), 16 bytes each."""
+    return N // 128 + min(B, N)
+
+
 def _check_plan(plan: torch.Tensor, B: int, N: int, device):
-    _check(plan, "plan", (load().fox_packed_plan_bytes(B, N) // 4,), torch.int32, device)
+    _need(plan, "plan", (_plan_places(B, N) * 4,), torch.int32, device)
 
 
 def _check_qkv(q, k, v):
@@ -36,8 +41,8 @@ def _check_qkv(q, k, v):
         raise ValueError(f"unsupported dtype {dt}")
     Hkv = k.shape[0]
     _check(q, "q", (H, N, d), dt, None)
-    _check(k, "k", (Hkv, N, d), dt, dev)
-    _check(v, "v", (Hkv, N, d), dt, dev)
+    _need(k, "k", (Hkv, N, d), dt, dev)
+    _need(v, "v", (Hkv, N, d), dt, dev)
     return H, Hkv, N, d
 
 
@@ -46,11 +51,9 @@ def fox_packed_plan(cu_seqlens: torch.Tensor, N: int) -> torch.Tensor:
     fox_attn_fwd_packed and fox_attn_bwd_packed of every layer."""
     B, dev = _check_cu(cu_seqlens, None), cu_seqlens.device
     lib = load()
-    nbytes = lib.fox_packed_plan_bytes(B, N)
-    plan = torch.empty(max(nbytes // 4, 4), device=dev, dtype=torch.int32)
-    with _on_device(dev):
-        st = lib.fox_packed_plan(_ptr(cu_seqlens), B, N, _ptr(plan), nbytes,
-                                 _raw_stream(dev.index))
+    places = _plan_places(B, N)
+    plan = torch.empty((places * 4,), device=dev, dtype=torch.int32)
+    st = _call(lib.fox_packed_plan, dev, _ptr(cu_seqlens), B, N, _ptr(plan), 16 * places)
     _raise(st, "fox_packed_plan")
     return plan
 
@@ -68,10 +71,9 @@ def fox_gate_prefix_packed(gate_logit: torch.Tensor, cu_seqlens: torch.Tensor,
     if c is None:
         c = torch.empty((H, N), device=dev, dtype=torch.float32)
     else:
-        _check(c, "c", (H, N), torch.float32, dev)
-    with _on_device(dev):
-        st = load().fox_gate_prefix_packed(_DT[dt], _ptr(gate_logit), _ptr(cu_seqlens), _ptr(c),
-                                           B, H, N, _raw_stream(dev.index))
+        _need(c, "c", (H, N), torch.float32, dev)
+    st = _call(load().fox_gate_prefix_packed, dev, _DT[dt], _ptr(gate_logit), _ptr(cu_seqlens),
+               _ptr(c), B, H, N)
     _raise(st, "fox_gate_prefix_packed")
     return c
 
@@ -86,7 +88,7 @@ def fox_attn_fwd_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c: to
     max_len: the longest sequence, if known.  Rows behind the last sequence are not written."""
     H, Hkv, N, d = _check_qkv(q, k, v)
     dev = q.device
-    _check(c, "c", (H, N), torch.float32, dev)
+    _need(c, "c", (H, N), torch.float32, dev)
     B = _check_cu(cu_seqlens, dev)
     if plan is None:
         plan = fox_packed_plan(cu_seqlens, N)
@@ -95,16 +97,14 @@ def fox_attn_fwd_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c: to
     if o is None:
         o = torch.empty_like(q)
     else:
-        _check(o, "o", (H, N, d), q.dtype, dev)
+        _need(o, "o", (H, N, d), q.dtype, dev)
     if lse is None:
         lse = torch.empty((H, N), device=dev, dtype=torch.float32)
     else:
-        _check(lse, "lse", (H, N), torch.float32, dev)
+        _need(lse, "lse", (H, N), torch.float32, dev)
     s = default_scale(d) if scale is None else float(scale)
-    with _on_device(dev):
-        st = load().fox_attn_fwd_packed(_DT[q.dtype], _ptr(q), _ptr(k), _ptr(v), _ptr(c),
-                                        _ptr(plan), _ptr(o), _ptr(lse), B, H, Hkv, N, d, max_len,
-                                        s, _raw_stream(dev.index))
+    st = _call(load().fox_attn_fwd_packed, dev, _DT[q.dtype], _ptr(q), _ptr(k), _ptr(v), _ptr(c),
+               _ptr(plan), _ptr(o), _ptr(lse), B, H, Hkv, N, d, max_len, s)
     _raise(st, "fox_attn_fwd_packed")
     return o, lse
 
@@ -123,13 +123,13 @@ def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
     H, Hkv, N, d = _check_qkv(q, k, v)
     dt, dev = q.dtype, q.device
     for name, t in (("o", o), ("d_o", d_o)):
-        _check(t, name, (H, N, d), dt, dev)
+        _need(t, name, (H, N, d), dt, dev)
     for name, t in (("c", c), ("lse", lse)):
-        _check(t, name, (H, N), torch.float32, dev)
+        _need(t, name, (H, N), torch.float32, dev)
     gdt = gate_logit.dtype
     if gdt not in _DT:
         raise ValueError(f"unsupported dtype {gdt}")
-    _check(gate_logit, "gate_logit", (H, N), gdt, dev)
+    _need(gate_logit, "gate_logit", (H, N), gdt, dev)
     B = _check_cu(cu_seqlens, dev)
     if plan is None:
         plan = fox_packed_plan(cu_seqlens, N)
@@ -139,23 +139,23 @@ def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
     d_logit = torch.empty_like(gate_logit) if d_logit is None else d_logit
-    _check(dq, "dq", (H, N, d), dt, dev)
-    _check(dk, "dk", (Hkv, N, d), dt, dev)
-    _check(dv, "dv", (Hkv, N, d), dt, dev)
-    _check(d_logit, "d_logit", (H, N), gdt, dev)
+    _need(dq, "dq", (H, N, d), dt, dev)
+    _need(dk, "dk", (Hkv, N, d), dt, dev)
+    _need(dv, "dv", (Hkv, N, d), dt, dev)
+    _need(d_logit, "d_logit", (H, N), gdt, dev)
     if d_log_f is not None:
-        _check(d_log_f, "d_log_f", (H, N), torch.float32, dev)
+        _need(d_log_f, "d_log_f", (H, N), torch.float32, dev)
     lib = load()
     if workspace is None:
-        workspace = _workspace(lib.fox_attn_bwd_packed_workspace_bytes(H, N), dev)
+        nbytes = lib.fox_attn_bwd_packed_workspace_bytes(H, N)
+        workspace = _workspace(nbytes, dev)
+    else:
+        nbytes = _workspace_bytes(workspace, dev)
     s = default_scale(d) if scale is None else float(scale)
-    with _on_device(dev):
-        st = lib.fox_attn_bwd_packed(
-            _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(o), _ptr(lse), _ptr(d_o), _DT[gdt],
-            _ptr(gate_logit), _ptr(cu_seqlens), _ptr(plan), _ptr(dq), _ptr(dk), _ptr(dv),
-            _ptr(d_logit), _ptr(d_log_f), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), B, H, Hkv, N, d, max_len, s,
-            _raw_stream(dev.index))
+    st = _call(lib.fox_attn_bwd_packed, dev, _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(o),
+               _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), _ptr(cu_seqlens), _ptr(plan),
+               _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_logit), _ptr(d_log_f), _ptr(workspace),
+               nbytes, B, H, Hkv, N, d, max_len, s)
     _raise(st, "fox_attn_bwd_packed")
     return dq, dk, dv, d_logit
 
@@ -166,10 +166,63 @@ def fox_packed_zero_behind(tensors: Sequence[torch.Tensor], cu_seqlens: torch.Te
     N = tensors[0].shape[1]
     rows = (_RowsStruct * len(tensors))()
     for i, t in enumerate(tensors):
-        _check(t, f"tensors[{i}]", (t.shape[0], N, *t.shape[2:]), None, dev)
+        _need(t, f"tensors[{i}]", (t.shape[0], N, *t.shape[2:]), None, dev)
         rows[i].x, rows[i].heads = _ptr(t), t.shape[0]
         rows[i].row_bytes = t[0, 0].numel() * t.element_size()
-    with _on_device(dev):
-        st = load().fox_packed_zero_behind(ctypes.addressof(rows), len(tensors),
-                                           _ptr(cu_seqlens), B, N, _raw_stream(dev.index))
+    st = _call(load().fox_packed_zero_behind, dev, ctypes.addressof(rows), len(tensors),
+               _ptr(cu_seqlens), B, N)
     _raise(st, "fox_packed_zero_behind")
+
+
+# ---------------------------------------------------------------------------
+# The two halves of an autograd step, each with one pass of checks.
+def _step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
+    """(plan, c, o, lse), o zero behind the last sequence."""
+    H, Hkv, N, d = _check_qkv(q, k, v)
+    dt, dev = _DT[q.dtype], q.device
+    gdt = gate_logit.dtype
+    if gdt not in _DT:
+        raise ValueError(f"unsupported dtype {gdt}")
+    _need(gate_logit, "gate_logit", (H, N), gdt, dev)
+    B = _check_cu(cu_seqlens, dev)
+    lib, cu = load(), _ptr(cu_seqlens)
+    if plan is None:
+        places = _plan_places(B, N)
+        plan = torch.empty((places * 4,), device=dev, dtype=torch.int32)
+        _raise(_call(lib.fox_packed_plan, dev, cu, B, N, _ptr(plan), 16 * places),
+               "fox_packed_plan")
+    else:
+        _check_plan(plan, B, N, dev)
+    c, lse = (torch.empty((H, N), device=dev, dtype=torch.float32) for _ in range(2))
+    o = torch.empty_like(q)
+    _raise(_call(lib.fox_gate_prefix_packed, dev, _DT[gdt], _ptr(gate_logit), cu, _ptr(c), B, H, N),
+           "fox_gate_prefix_packed")
+    _raise(_call(lib.fox_attn_fwd_packed, dev, dt, _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(plan),
+                 _ptr(o), _ptr(lse), B, H, Hkv, N, d, max_len, scale), "fox_attn_fwd_packed")
+    row = _RowsStruct(_ptr(o), H, d * o.element_size())
+    _raise(_call(lib.fox_packed_zero_behind, dev, ctypes.addressof(row), 1, cu, B, N),
+           "fox_packed_zero_behind")
+    return plan, c, o, lse
+
+
+def _step_backward(saved, d_o, max_len, scale):
+    """dq, dk, dv, d_logit, zero behind the last sequence, from what the forward checked."""
+    q, k, v, gate_logit, c, o, lse, cu_seqlens, plan = saved
+    (H, N, d), Hkv, B = q.shape, k.shape[0], cu_seqlens.shape[0] - 1
+    dt, gdt, dev = q.dtype, gate_logit.dtype, q.device
+    _need(d_o, "d_o", (H, N, d), dt, dev)
+    lib, cu = load(), _ptr(cu_seqlens)
+    grads = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v),
+             torch.empty_like(gate_logit))
+    nbytes = lib.fox_attn_bwd_packed_workspace_bytes(H, N)
+    ws = _workspace(nbytes, dev)
+    _raise(_call(lib.fox_attn_bwd_packed, dev, _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c),
+                 _ptr(o), _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), cu, _ptr(plan),
+                 *map(_ptr, grads), None, _ptr(ws), nbytes, B, H, Hkv, N, d, max_len, scale),
+           "fox_attn_bwd_packed")
+    e, ge = q.element_size(), gate_logit.element_size()
+    rows = (_RowsStruct * 4)((_ptr(grads[0]), H, d * e), (_ptr(grads[1]), Hkv, d * e),
+                             (_ptr(grads[2]), Hkv, d * e), (_ptr(grads[3]), H, ge))
+    _raise(_call(lib.fox_packed_zero_behind, dev, ctypes.addressof(rows), 4, cu, B, N),
+           "fox_packed_zero_behind")
+    return grads

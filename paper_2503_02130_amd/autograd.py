@@ -62,22 +62,17 @@ class PackedForgettingAttention(torch.autograd.Function):
     def forward(ctx, q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
         gate_logit = gate_logit.contiguous()
-        if plan is None:
-            plan = _packed.fox_packed_plan(cu_seqlens, q.shape[1])
-        c = _packed.fox_gate_prefix_packed(gate_logit, cu_seqlens)
-        o, lse = _packed.fox_attn_fwd_packed(q, k, v, c, cu_seqlens, plan, max_len, scale)
-        _packed.fox_packed_zero_behind((o,), cu_seqlens)
+        plan, c, o, lse = _packed._step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len,
+                                                scale)
         ctx.save_for_backward(q, k, v, gate_logit, c, o, lse, cu_seqlens, plan)
         ctx.max_len, ctx.scale = max_len, scale
         return o
 
     @staticmethod
     def backward(ctx, d_o):
-        q, k, v, gate_logit, c, o, lse, cu_seqlens, plan = ctx.saved_tensors
-        d_o = d_o.to(q.dtype).contiguous()
-        grads = _packed.fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit, cu_seqlens,
-                                            plan, ctx.max_len, ctx.scale)
-        _packed.fox_packed_zero_behind(grads, cu_seqlens)
+        saved = ctx.saved_tensors
+        grads = _packed._step_backward(saved, d_o.to(saved[0].dtype).contiguous(), ctx.max_len,
+                                       ctx.scale)
         return (*grads, None, None, None, None)
 
 

@@ -893,7 +893,8 @@ fox_status_t fox_cache_keep(const fox_cache_t* cache, const int* seq_len, const 
 }
 
 fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const int* start,
-                   const int* seq_len, void* k, void* v, float* c, int T, hipStream_t stream) {
+                   const int* seq_len, void* k, void* v, float* c, int T, int zero_others,
+                   hipStream_t stream) {
   fox_status_t st = check_cache(cache);
   if (st) return st;
   if (!all_set({seq_len, k, v})) return FOX_ERR_NULL;
@@ -901,7 +902,7 @@ fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const i
   if (!cache_dtype(dtype)) return FOX_ERR_UNSUPPORTED;
   if (!all_aligned16({start, seq_len, k, v, c})) return FOX_ERR_ALIGN;
   return launch_status(fox::launch_cache_read(cache_spec(cache), dtype == FOX_DTYPE_BF16, start,
-                                              seq_len, k, v, c, T, stream));
+                                              seq_len, k, v, c, T, zero_others != 0, stream));
 }
 
 size_t fox_attn_cache_workspace_bytes(const fox_cache_t* cache, int n, int max_len) {

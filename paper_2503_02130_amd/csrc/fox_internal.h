@@ -205,7 +205,7 @@ hipError_t launch_cache_append_packed(const CacheSpec& s, bool bf16, const void*
 hipError_t launch_cache_keep(const CacheSpec& s, const int* seq_len, const int* index,
                              const int* n_keep, int n, hipStream_t st);
 hipError_t launch_cache_read(const CacheSpec& s, bool bf16, const int* start, const int* seq_len,
-                             void* k, void* v, float* c, int T, hipStream_t st);
+                             void* k, void* v, float* c, int T, bool zero_others, hipStream_t st);
 size_t attn_cache_workspace_bytes(const CacheSpec& s, int n, int max_len);
 hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_len,
                              const int* parent, const int* n_new, void* o, float* lse, void* ws,

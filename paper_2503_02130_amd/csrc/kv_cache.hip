@@ -306,15 +306,22 @@ __device__ __forceinline__ void get_row(const void* src, const uint8_t* exps, si
 template <typename T, int D, bool F8>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(
     CacheView cv, const int* __restrict__ start, const int* __restrict__ seq_len,
-    T* __restrict__ k, T* __restrict__ v, float* __restrict__ c, int T_, unsigned gate_groups) {
+    T* __restrict__ k, T* __restrict__ v, float* __restrict__ c, int T_, bool zero_others,
+    unsigned gate_groups) {
+  // the page of row t of sequence b, -1 where it has no token
+  auto page = [&](int b, int t, int& slot) {
+    const int s0 = start ? max(start[b], 0) : 0;
+    slot = cv.slot_of(s0 + t);
+    return t < max(seq_len[b], 0) - s0 ? cv.page_of(b, s0 + t) : -1;
+  };
+  int slot;
   if (blockIdx.x < gate_groups) {
     const long long i = (long long)blockIdx.x * kCacheThreads + threadIdx.x;
     if (i >= (long long)cv.B * cv.H * T_) return;
     const int t = (int)(i % T_), h = (int)(i / T_ % cv.H), b = (int)(i / T_ / cv.H);
-    const int s0 = start ? max(start[b], 0) : 0;
-    if (t >= max(seq_len[b], 0) - s0) return;
-    const int p = cv.page_of(b, s0 + t);
-    if (p >= 0) c[i] = cv.c[cv.c_at(p, h, cv.slot_of(s0 + t))];
+    const int p = page(b, t, slot);
+    if (p >= 0) c[i] = cv.c[cv.c_at(p, h, slot)];
+    else if (zero_others) c[i] = 0.0f;
     return;
   }
   constexpr int LPR = D / 8, RPB = kCacheThreads / LPR;
@@ -322,13 +329,17 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(
   const long long r = (long long)(blockIdx.x - gate_groups) * RPB + threadIdx.x / LPR;
   if (r >= (long long)cv.B * cv.Hkv * T_) return;
   const int t = (int)(r % T_), h = (int)(r / T_ % cv.Hkv), b = (int)(r / T_ / cv.Hkv);
-  const int s0 = start ? max(start[b], 0) : 0;
-  if (t >= max(seq_len[b], 0) - s0) return;
-  const int p = cv.page_of(b, s0 + t);
-  if (p < 0) return;
-  const size_t row = cv.kv_row(p, h, cv.slot_of(s0 + t));
-  get_row<T, D, F8>(cv.k, cv.ke, row, part, k + (size_t)r * D + 8 * part);
-  get_row<T, D, F8>(cv.v, cv.ve, row, part, v + (size_t)r * D + 8 * part);
+  const int p = page(b, t, slot);
+  T *ko = k + (size_t)r * D + 8 * part, *vo = v + (size_t)r * D + 8 * part;
+  if (p >= 0) {
+    const size_t row = cv.kv_row(p, h, slot);
+    get_row<T, D, F8>(cv.k, cv.ke, row, part, ko);
+    get_row<T, D, F8>(cv.v, cv.ve, row, part, vo);
+  } else if (zero_others) {
+    const float zeros[8] = {};
+    store8(ko, zeros);
+    store8(vo, zeros);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -390,14 +401,14 @@ hipError_t launch_cache_keep(const CacheSpec& s, const int* seq_len, const int* 
 }
 
 hipError_t launch_cache_read(const CacheSpec& s, bool bf16_, const int* start, const int* seq_len,
-                             void* k, void* v, float* c, int T_, hipStream_t st) {
+                             void* k, void* v, float* c, int T_, bool zero_others, hipStream_t st) {
   const unsigned gates = c ? groups_of((long long)s.B * s.H * T_, kCacheThreads) : 0;
   const unsigned rows = groups_of((long long)s.B * s.Hkv * T_, kCacheThreads / (s.d / 8));
   cache_dispatch(s, bf16_, [&](auto tag, auto dc, auto f8) {
     typedef std::remove_pointer_t<decltype(tag)> T;
     hipLaunchKernelGGL((cache_read_kernel<T, decltype(dc)::value, decltype(f8)::value>),
                        dim3(gates + rows), dim3(kCacheThreads), 0, st, cache_view(s), start, seq_len,
-                       (T*)k, (T*)v, c, T_, gates);
+                       (T*)k, (T*)v, c, T_, zero_others, gates);
   });
   return hipGetLastError();
 }
