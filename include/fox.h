@@ -539,7 +539,7 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  * fox_attn_bwd_packed: the gradients of sum(O o dO): dq, dk, dv (dk, dv summed over the query
  *   heads of a key head) and d_logit in gate_dtype, the gradient of the gate logits; d_log_f
  *   [H,N] fp32, that of log f, may be NULL.  workspace: at least
- *   fox_attn_bwd_packed_workspace_bytes().
+ *   fox_attn_bwd_packed_workspace_bytes() for the same max_len.
  * fox_packed_zero_behind: writes zeros to the rows behind the last sequence of n (at most 8)
  *   tensors [heads, N, row_bytes] on the device; row_bytes even.
  */
@@ -558,7 +558,8 @@ fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_log
 fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
                         const float* c, const void* plan, void* o, float* lse, int B, int H,
                         int H_kv, int N, int d, int max_len, float scale, hipStream_t stream);
-size_t fox_attn_bwd_packed_workspace_bytes(int H, int N);
+size_t fox_attn_bwd_packed_workspace_bytes(fox_dtype_t dtype, int H, int H_kv, int N, int d,
+                                           int max_len);
 fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
                         const float* c, const void* o, const float* lse, const void* d_o,
                         fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,

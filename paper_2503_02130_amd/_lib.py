@@ -186,7 +186,7 @@ def load() -> ctypes.CDLL:
     lib.fox_packed_plan_bytes.restype = Z
     lib.fox_packed_plan_bytes.argtypes = [I, I]
     lib.fox_attn_bwd_packed_workspace_bytes.restype = Z
-    lib.fox_attn_bwd_packed_workspace_bytes.argtypes = [I, I]
+    lib.fox_attn_bwd_packed_workspace_bytes.argtypes = [I, I, I, I, I, I]
     lib.fox_attn_cache_workspace_bytes.restype = Z
     lib.fox_attn_cache_workspace_bytes.argtypes = [P, I, I]
     _lib = lib

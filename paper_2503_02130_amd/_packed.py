@@ -109,8 +109,9 @@ def fox_attn_fwd_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c: to
     return o, lse
 
 
-def fox_attn_bwd_packed_workspace_bytes(H: int, N: int) -> int:
-    return int(load().fox_attn_bwd_packed_workspace_bytes(H, N))
+def fox_attn_bwd_packed_workspace_bytes(dtype: torch.dtype, H: int, H_kv: int, N: int, d: int,
+                                        max_len: int = 0) -> int:
+    return int(load().fox_attn_bwd_packed_workspace_bytes(_DT[dtype], H, H_kv, N, d, max_len))
 
 
 def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
@@ -147,7 +148,7 @@ def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
         _need(d_log_f, "d_log_f", (H, N), torch.float32, dev)
     lib = load()
     if workspace is None:
-        nbytes = lib.fox_attn_bwd_packed_workspace_bytes(H, N)
+        nbytes = lib.fox_attn_bwd_packed_workspace_bytes(_DT[dt], H, Hkv, N, d, max_len)
         workspace = _workspace(nbytes, dev)
     else:
         nbytes = _workspace_bytes(workspace, dev)
@@ -214,7 +215,7 @@ def _step_backward(saved, d_o, max_len, scale):
     lib, cu = load(), _ptr(cu_seqlens)
     grads = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v),
              torch.empty_like(gate_logit))
-    nbytes = lib.fox_attn_bwd_packed_workspace_bytes(H, N)
+    nbytes = lib.fox_attn_bwd_packed_workspace_bytes(_DT[dt], H, Hkv, N, d, max_len)
     ws = _workspace(nbytes, dev)
     _raise(_call(lib.fox_attn_bwd_packed, dev, _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c),
                  _ptr(o), _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), cu, _ptr(plan),

@@ -172,6 +172,8 @@ __device__ __forceinline__ f32x4 f32_get_partial(const char* slice, int row, int
 struct F32Packed {
   const PackedItem* plan;
   int n_items, H, Hkv, N;
+  int splits;   // dK, dV: groups that a key head's query heads are split into, and their
+  float* part;  // partial sums [group][dK, dV][Hkv][N][D]
 };
 struct F32Place {
   int bh, mb, L;
@@ -485,21 +487,24 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
   const uint32_t dma_off = f32_dma_offset<D>(lane);
   const F32Reads<D> qt(sm.tile[wave][0], col, h), gt(sm.tile[wave][1], col, h);
   const lds_byte* row_at = lds_opaque(lds_ptr(&sm.row[wave][0][4 * h]));
-  const int G = PK ? pk.H / pk.Hkv : 1;
-  const long long n_all = f32_blocks<PK>(n_blk, BH, pk, pk.Hkv);
+  const int G = PK ? pk.H / pk.Hkv / pk.splits : 1;  // query heads of this workgroup
+  const long long n_all = f32_blocks<PK>(n_blk, BH, pk, pk.Hkv * pk.splits);
 
   for (long long blk = blockIdx.x; blk < n_all; blk += gridDim.x) {
     int bh = (int)(blk % BH), L = L_;
     int kb = (int)(blk / BH);  // key block 0 has the most work: first
     size_t head = (size_t)bh * (size_t)L, kv_row = head;
+    int hg = 0;
     if constexpr (PK) {
       // an item's block m, as keys, is block n - 1 - m of the sequence's n
-      const PackedItem it = pk.plan[blk / (4 * pk.Hkv)];
-      const int i = (int)(blk % (4 * pk.Hkv)), hk = i % pk.Hkv;
+      const int per = pk.Hkv * pk.splits;
+      const PackedItem it = pk.plan[blk / (4 * per)];
+      const int i = (int)(blk % (4 * per)), hk = i % pk.Hkv;
+      hg = i / pk.Hkv % pk.splits;
       L = it.len;
-      kb = 4 * ((L + kPackedBlock - 1) / kPackedBlock - 1 - it.block) + i / pk.Hkv;
+      kb = 4 * ((L + kPackedBlock - 1) / kPackedBlock - 1 - it.block) + i / per;
       if (L <= 0 || 32 * kb >= L) continue;
-      bh = hk * G;
+      bh = (hk * pk.splits + hg) * G;
       head = (size_t)bh * pk.N + it.start;
       kv_row = (size_t)hk * pk.N + it.start;
     }
@@ -596,7 +601,13 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
         ov += f32_get_partial<D>(sm.tile[w][1], kr, chunk);
         dt += sm.dc[w][kr];
       }
-      if (k0 + kr < L) {
+      if (PK && pk.splits > 1) {
+        if (k0 + kr < L) {
+          const size_t at = ((size_t)hg * 2 * pk.Hkv * pk.N + kv_row + k0 + kr) * D + 4 * chunk;
+          *reinterpret_cast<f32x4*>(pk.part + at) = ok * scale;
+          *reinterpret_cast<f32x4*>(pk.part + at + (size_t)pk.Hkv * pk.N * D) = ov;
+        }
+      } else if (k0 + kr < L) {
         *reinterpret_cast<f32x4*>(dK + (kv_row + k0 + kr) * D + 4 * chunk) = ok * scale;
         *reinterpret_cast<f32x4*>(dV + (kv_row + k0 + kr) * D + 4 * chunk) = ov;
         if (!PK && chunk == 0) dck[head + k0 + kr] = dt;
@@ -726,7 +737,7 @@ static void packed_fwd_f32_t(const float* q, const float* k, const float* v, con
 hipError_t launch_packed_fwd_f32(const float* q, const float* k, const float* v, const float* c,
                                  float* o, float* lse, const void* plan, int B, int H, int Hkv,
                                  int N, int d, float scale, hipStream_t s) {
-  const F32Packed pk{static_cast<const PackedItem*>(plan), packed_items(B, N), H, Hkv, N};
+  const F32Packed pk{static_cast<const PackedItem*>(plan), packed_items(B, N), H, Hkv, N, 1, nullptr};
   if (d == 128) packed_fwd_f32_t<128, 4>(q, k, v, c, o, lse, pk, scale * kLog2e, s);
   else packed_fwd_f32_t<64, 8>(q, k, v, c, o, lse, pk, scale * kLog2e, s);
   return hipGetLastError();
@@ -737,7 +748,8 @@ static void packed_bwd_f32_t(const float* q, const float* k, const float* v, con
                              const float* lse, const float* d_o, const float* delta, float* dq,
                              float* dk, float* dv, float* dcq, float* dck, const F32Packed& pk,
                              float scale, hipStream_t s) {
-  const long long q_blocks = 4LL * pk.n_items * pk.H, k_blocks = 4LL * pk.n_items * pk.Hkv;
+  const long long q_blocks = 4LL * pk.n_items * pk.H;
+  const long long k_blocks = 4LL * pk.n_items * pk.Hkv * pk.splits;
   auto kv = [&](auto kernel, int nw) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(k_blocks, kF32MaxGrid)), dim3(64 * nw), 0, s,
                        q, k, v, c, lse, d_o, delta, dk, dv, dck, 1, 1, 0, 0, scale, scale * kLog2e,
@@ -756,15 +768,17 @@ static void packed_bwd_f32_t(const float* q, const float* k, const float* v, con
 hipError_t launch_packed_bwd_f32(const float* q, const float* k, const float* v, const float* c,
                                  const float* o, const float* lse, const float* d_o, float* dq,
                                  float* dk, float* dv, float* delta, float* dcq, float* dck,
-                                 const void* plan, int B, int H, int Hkv, int N, int d,
-                                 float scale, hipStream_t s) {
+                                 float* part, const void* plan, const int* cu, int B, int H,
+                                 int Hkv, int N, int d, int max_len, float scale, hipStream_t s) {
   const hipError_t e = launch_bwd_delta(false, o, d_o, delta, H, N, d, s);
   if (e != hipSuccess) return e;
-  const F32Packed pk{static_cast<const PackedItem*>(plan), packed_items(B, N), H, Hkv, N};
+  const int splits = packed_head_split(false, H, Hkv, N, d, max_len);
+  const F32Packed pk{static_cast<const PackedItem*>(plan), packed_items(B, N), H, Hkv, N, splits, part};
   if (d == 128)
     packed_bwd_f32_t<128, 4>(q, k, v, c, lse, d_o, delta, dq, dk, dv, dcq, dck, pk, scale, s);
   else
     packed_bwd_f32_t<64, 8>(q, k, v, c, lse, d_o, delta, dq, dk, dv, dcq, dck, pk, scale, s);
+  if (splits > 1) return launch_packed_head_sum(false, part, cu, dk, dv, B, Hkv, N, d, splits, s);
   return hipGetLastError();
 }
 

@@ -14,8 +14,10 @@
 //   * The workgroups of an item's heads are numbered so that an XCD sees few key heads: the G
 //     query heads of a key head read the same K and V from its L2.
 //   * dK and dV of a key block sum over the G query heads in one workgroup's registers: the
-//     loop walks the query tiles of one head after the other (no atomics, no partial sums in
-//     memory).  dc^k, which belongs to a query head, is written as each head ends.
+//     loop walks the query tiles of one head after the other (no atomics).  Where the longest
+//     such walk would decide the time, the heads are split over workgroups whose fp32 partial
+//     sums are added up afterwards (packed_head_split).  dc^k, which belongs to a query head,
+//     is written as each head ends.
 //   * The row sum l adds the unrounded fp32 P, and dc^q, dc^k the unrounded fp32 dS (of P as
 //     rounded to bf16 in both kernels, so that they are sums of one matrix): LSE is then an
 //     fp32 quantity to its last digits, and d(log f), a long sum of differences, keeps the
@@ -676,18 +678,20 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
                         const bf16* __restrict__ V, const float* __restrict__ C,
                         const float* __restrict__ LSE, const bf16* __restrict__ dO,
                         const float* __restrict__ delta, bf16* __restrict__ dK,
-                        bf16* __restrict__ dV, float* __restrict__ dck,
-                        const PackedItem* __restrict__ plan, int H, int Hkv, int N, float scale,
-                        float scale_log2) {
+                        bf16* __restrict__ dV, float* __restrict__ dck, float* __restrict__ part,
+                        const PackedItem* __restrict__ plan, int H, int Hkv, int splits, int N,
+                        float scale, float scale_log2) {
   constexpr int NQB = BM / 32;
   constexpr int TILE = BM * D;
   constexpr int NDMA = TILE * 2 / 1024 / kPkPairs;
   static_assert(NDMA >= 1 && NDMA * kPkPairs * 1024 == TILE * 2, "the P waves cover a tile");
   __shared__ __attribute__((aligned(16))) PkKvSmem<D, BM> sm;
 
-  const PackedItem item = plan[blockIdx.x / Hkv];
+  const PackedItem item = plan[blockIdx.x / (Hkv * splits)];
   if (item.len <= 0) return;
-  const int L = item.len, hk = (int)(blockIdx.x % Hkv), G = H / Hkv;
+  // the query heads of this workgroup: group hg of G heads of the key head's
+  const int L = item.len, hk = (int)(blockIdx.x % Hkv), hg = (int)(blockIdx.x / Hkv % splits);
+  const int G = H / Hkv / splits;
   // the item of a sequence's block m does the work of m + 1 blocks; as keys, that is block
   // n_blocks - 1 - m
   const int k0 = ((L + kPackedBlock - 1) / kPackedBlock - 1 - item.block) * kPackedBlock;
@@ -695,7 +699,7 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   const int h = lane >> 5, col = lane & 31;
   const bool pwave = wave < kPkPairs;
   const int pair = wave % kPkPairs;
-  const size_t head0 = (size_t)hk * G * N + item.start;  // row of the sequence in head hk G
+  const size_t head0 = ((size_t)hk * splits + hg) * G * N + item.start;
   const size_t kv_row = (size_t)hk * N + item.start;
   const int kw0 = k0 + pair * 32;
   const int kj = kw0 + col;
@@ -942,9 +946,21 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
     step(it + 2, std::integral_constant<int, 2>());
   }
 
-  if (k_valid) {
+  const float f = pwave ? 1.0f : scale;
+  if (splits > 1) {
+    // partial dK and dV of these heads: [group][dK, dV][Hkv][N][D]
+    if (k_valid) {
+      float* out = part + (((size_t)hg * 2 + (pwave ? 1 : 0)) * Hkv * N + kv_row + kj) * D;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4*>(out + db * 32 + 8 * g + 4 * h) =
+              f32x4{acc[db][4 * g] * f, acc[db][4 * g + 1] * f, acc[db][4 * g + 2] * f,
+                    acc[db][4 * g + 3] * f};
+    }
+  } else if (k_valid) {
     bf16* out = (pwave ? dV : dK) + (kv_row + kj) * D;
-    const float f = pwave ? 1.0f : scale;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -955,6 +971,69 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
         *reinterpret_cast<bf16x4*>(out + db * 32 + 8 * g + 4 * h) = w;
       }
   }
+}
+
+// dK and dV from the partial sums of `splits` groups of heads, in the order of the groups; rows
+// behind the last sequence (no partial sums) are left as they were.
+template <typename T>
+__global__ __launch_bounds__(256) void packed_head_sum_kernel(const float* __restrict__ part,
+                                                              const int* __restrict__ cu,
+                                                              T* __restrict__ dK, T* __restrict__ dV,
+                                                              int B, int Hkv, int N, int d,
+                                                              int splits) {
+  const size_t n4 = (size_t)Hkv * N * d / 4;  // pieces of four of one tensor
+  const int end = min(max(cu[B], 0), N);
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < 2 * n4; i += (size_t)gridDim.x * 256) {
+    const size_t at = i < n4 ? i : i - n4;
+    if ((int)(at / (d / 4) % N) >= end) continue;
+    f32x4 sum = reinterpret_cast<const f32x4*>(part)[i];
+    for (int s = 1; s < splits; ++s) sum += reinterpret_cast<const f32x4*>(part)[(size_t)s * 2 * n4 + i];
+    T* out = (i < n4 ? dK : dV) + 4 * at;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<bf16x4*>(out) =
+          bf16x4{to_bf16(sum[0]), to_bf16(sum[1]), to_bf16(sum[2]), to_bf16(sum[3])};
+    } else {
+      *reinterpret_cast<f32x4*>(out) = sum;
+    }
+  }
+}
+
+hipError_t launch_packed_head_sum(bool bf16_, const float* part, const int* cu, void* dk, void* dv,
+                                  int B, int Hkv, int N, int d, int splits, hipStream_t s) {
+  const size_t n = (size_t)Hkv * N * d / 2;
+  const dim3 grid((unsigned)std::min<size_t>((n + 255) / 256, 4096));
+  if (bf16_)
+    hipLaunchKernelGGL(packed_head_sum_kernel<bf16>, grid, dim3(256), 0, s, part, cu, (bf16*)dk,
+                       (bf16*)dv, B, Hkv, N, d, splits);
+  else
+    hipLaunchKernelGGL(packed_head_sum_kernel<float>, grid, dim3(256), 0, s, part, cu, (float*)dk,
+                       (float*)dv, B, Hkv, N, d, splits);
+  return hipGetLastError();
+}
+
+// Groups that the query heads of a key head are split into for dK and dV, a divisor of G.  A
+// workgroup walks G / groups heads times the query tiles behind its keys, so the time is about
+// the larger of the longest sequence's walk and the mean load of the part, and each split
+// writes and reads fp32 sums.  In steps of 128 x 128 scores (bf16: about 3.7 us, one or two
+// workgroups per CU at D = 128 and 64; fp32: 32 rows and NW waves, about 8 us per 32 x 32 of
+// each wave).
+int packed_head_split(bool bf16_, int H, int Hkv, int N, int d, int max_len) {
+  const int G = H / Hkv;
+  const double rows = bf16_ ? 128 : 32, waves = bf16_ ? 1 : d == 64 ? 8 : 4;
+  const double chain = std::max(1.0, max_len / rows / waves), step_us = bf16_ ? 3.7 : 8.0;
+  const double mean = (double)H * (N / rows) * (chain + 1) / 2 / (bf16_ && d == 64 ? 512 : 256);
+  int best = 1;
+  double best_us = 0.0;
+  for (int s = 1; s <= G; ++s) {
+    if (G % s) continue;
+    const double sums = s == 1 ? 0.0 : 5.0 + (double)s * Hkv * N * d * 16 / 4e6;
+    const double us = std::max(G / s * chain, mean) * step_us + sums;
+    if (s == 1 || us < best_us) {
+      best = s;
+      best_us = us;
+    }
+  }
+  return best;
 }
 
 // ---------------------------------------------------------------------------
@@ -976,16 +1055,18 @@ hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const 
 
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
                              const void* o, const float* lse, const void* d_o, void* dq, void* dk,
-                             void* dv, float* delta, float* dcq, float* dck, const void* plan,
-                             int B, int H, int Hkv, int N, int d, int max_len, float scale,
-                             hipStream_t s) {
+                             void* dv, float* delta, float* dcq, float* dck, float* part,
+                             const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
+                             int max_len, float scale, hipStream_t s) {
   hipError_t e = launch_bwd_delta(true, o, d_o, delta, H, N, d, s);
   if (e != hipSuccess) return e;
   const unsigned items = (unsigned)packed_items(B, N);
+  const int splits = packed_head_split(true, H, Hkv, N, d, max_len);
   auto kv = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(items * Hkv), dim3(kPkKvThreads), 0, s, (const bf16*)q,
+    hipLaunchKernelGGL(kernel, dim3(items * Hkv * splits), dim3(kPkKvThreads), 0, s, (const bf16*)q,
                        (const bf16*)k, (const bf16*)v, c, lse, (const bf16*)d_o, delta, (bf16*)dk,
-                       (bf16*)dv, dck, (const PackedItem*)plan, H, Hkv, N, scale, scale * kLog2e);
+                       (bf16*)dv, dck, part, (const PackedItem*)plan, H, Hkv, splits, N, scale,
+                       scale * kLog2e);
   };
   auto qs = [&](auto kernel, int groups) {
     hipLaunchKernelGGL(kernel, dim3(items * H), dim3(kPkThreads * groups), 0, s, (const bf16*)q,
@@ -999,6 +1080,7 @@ hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const 
     kv(packed_dkdv_kernel<64, 32>);
     qs(packed_dq_kernel<64, 1>, 1);
   }
+  if (splits > 1) return launch_packed_head_sum(true, part, cu, dk, dv, B, Hkv, N, d, splits, s);
   return hipGetLastError();
 }
 

@@ -971,9 +971,13 @@ fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k
                                                   H_kv, N, d, scale, stream));
 }
 
-size_t fox_attn_bwd_packed_workspace_bytes(int H, int N) {
-  if (check_packed(1, H, H, N)) return 0;
-  return (size_t)3 * H * N * sizeof(float) + 32;
+size_t fox_attn_bwd_packed_workspace_bytes(fox_dtype_t dtype, int H, int H_kv, int N, int d,
+                                           int max_len) {
+  if (check_packed(1, H, H_kv, N) || check_dtype_d(dtype, d)) return 0;
+  const int len = max_len <= 0 || max_len > N ? N : max_len;
+  const int splits = fox::packed_head_split(dtype == FOX_DTYPE_BF16, H, H_kv, N, d, len);
+  const size_t row = ((size_t)H * N + 3) & ~(size_t)3;  // delta, dc_q, dc_k
+  return (3 * row + (splits > 1 ? (size_t)splits * 2 * H_kv * N * d : 0)) * sizeof(float);
 }
 
 fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
@@ -993,22 +997,23 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
   if (!all_aligned16({q, k, v, c, o, lse, d_o, gate_logit, cu_seqlens, plan, dq, dk, dv, d_logit,
                       d_log_f, workspace}))
     return FOX_ERR_ALIGN;
-  if (!workspace || workspace_bytes < fox_attn_bwd_packed_workspace_bytes(H, N))
+  if (!workspace ||
+      workspace_bytes < fox_attn_bwd_packed_workspace_bytes(dtype, H, H_kv, N, d, max_len))
     return FOX_ERR_WORKSPACE;
   const int len = max_len <= 0 || max_len > N ? N : max_len;
   // delta, dc_q, dc_k, each on a 16-byte boundary
   const size_t row = ((size_t)H * N + 3) & ~(size_t)3;
   float* delta = static_cast<float*>(workspace);
-  float *dcq = delta + row, *dck = dcq + row;
+  float *dcq = delta + row, *dck = dcq + row, *part = dck + row;
   hipError_t e;
   if (dtype == FOX_DTYPE_BF16)
-    e = fox::launch_packed_bwd(q, k, v, c, o, lse, d_o, dq, dk, dv, delta, dcq, dck, plan, B, H,
-                               H_kv, N, d, len, scale, stream);
+    e = fox::launch_packed_bwd(q, k, v, c, o, lse, d_o, dq, dk, dv, delta, dcq, dck, part, plan,
+                               cu_seqlens, B, H, H_kv, N, d, len, scale, stream);
   else
     e = fox::launch_packed_bwd_f32((const float*)q, (const float*)k, (const float*)v, c,
                                    (const float*)o, lse, (const float*)d_o, (float*)dq, (float*)dk,
-                                   (float*)dv, delta, dcq, dck, plan, B, H, H_kv, N, d, scale,
-                                   stream);
+                                   (float*)dv, delta, dcq, dck, part, plan, cu_seqlens, B, H,
+                                   H_kv, N, d, len, scale, stream);
   if (e == hipSuccess)
     e = fox::launch_packed_gate_grad(gate_dtype == FOX_DTYPE_BF16, dcq, dck, gate_logit,
                                      cu_seqlens, d_log_f, d_logit, B, H, N, stream);

@@ -230,19 +230,24 @@ hipError_t launch_packed_zero(const ZeroRows* x, int n, const int* cu, int B, in
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
                              float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s);
+// Groups that the query heads of a key head are split into for dK and dV; with more than one,
+// `part` holds their partial sums, fp32 [groups][2][Hkv][N][d].
+int packed_head_split(bool bf16, int H, int Hkv, int N, int d, int max_len);
+hipError_t launch_packed_head_sum(bool bf16, const float* part, const int* cu, void* dk, void* dv,
+                                  int B, int Hkv, int N, int d, int splits, hipStream_t s);
 // dq, dk, dv, dc_q and dc_k (delta: [H, N] scratch)
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
                              const void* o, const float* lse, const void* d_o, void* dq, void* dk,
-                             void* dv, float* delta, float* dcq, float* dck, const void* plan,
-                             int B, int H, int Hkv, int N, int d, int max_len, float scale,
-                             hipStream_t s);
+                             void* dv, float* delta, float* dcq, float* dck, float* part,
+                             const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
+                             int max_len, float scale, hipStream_t s);
 hipError_t launch_packed_fwd_f32(const float* q, const float* k, const float* v, const float* c,
                                  float* o, float* lse, const void* plan, int B, int H, int Hkv,
                                  int N, int d, float scale, hipStream_t s);
 hipError_t launch_packed_bwd_f32(const float* q, const float* k, const float* v, const float* c,
                                  const float* o, const float* lse, const float* d_o, float* dq,
                                  float* dk, float* dv, float* delta, float* dcq, float* dck,
-                                 const void* plan, int B, int H, int Hkv, int N, int d,
-                                 float scale, hipStream_t s);
+                                 float* part, const void* plan, const int* cu, int B, int H,
+                                 int Hkv, int N, int d, int max_len, float scale, hipStream_t s);
 
 }  // namespace fox

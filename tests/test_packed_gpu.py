@@ -251,7 +251,7 @@ def test_step_in_a_graph():
         e = torch.empty_like
         return (dict(o=e(q), lse=torch.empty((H, N), device=DEV), dq=e(q), dk=e(k), dv=e(v),
                      d_logit=e(logit)),
-                torch.empty(fox.fox_attn_bwd_packed_workspace_bytes(H, N), device=DEV,
+                torch.empty(fox.fox_attn_bwd_packed_workspace_bytes(BF, H, Hkv, N, d), device=DEV,
                             dtype=torch.uint8))
 
     (outs, ws), (want, ws2) = buffers(), buffers()
