@@ -18,10 +18,14 @@
 //     such walk would decide the time, the heads are split over workgroups whose fp32 partial
 //     sums are added up afterwards (packed_head_split).  dc^k, which belongs to a query head,
 //     is written as each head ends.
-//   * The row sum l adds the unrounded fp32 P, and dc^q, dc^k the unrounded fp32 dS (of P as
-//     rounded to bf16 in both kernels, so that they are sums of one matrix): LSE is then an
-//     fp32 quantity to its last digits, and d(log f), a long sum of differences, keeps the
-//     accuracy of P.
+//   * The row sum l adds the unrounded fp32 P, so that LSE is an fp32 quantity to its last
+//     digits.  The backward forms dS from P rounded to fp16 (2^-12 of it; carried as 2^15 P,
+//     which fp16 holds to full precision down to 2^-29) and dc^k adds the unrounded fp32 dS.
+//   * c_i shifts a whole softmax row, so dc^q = rowsum(dS) is 0; what it comes out as is the
+//     error of Delta, formed from O as rounded to bf16.  The dQ kernel runs first and adds its
+//     row sums (of dS in fp32) to Delta: the dK/dV kernel then sees the Delta of its own P,
+//     rows of dS that sum to 0 to fp32 rounding, and d(log f) is the reverse sum of dc^k
+//     alone.  bf16 rounding is left in the operands dS and, for dV, P.
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>
@@ -386,11 +390,27 @@ void packed_fwd_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
 }
 
 // ---------------------------------------------------------------------------
-// dQ and dc^q
+// dQ, and Delta from dc^q
 // ---------------------------------------------------------------------------
-// Both backward kernels form P from the same expression, so that its bf16 roundings agree:
-// the bias is relative to c at the start of the key's aligned block of kPkRef keys.
+// Both backward kernels form P from the same expression, so that its roundings agree: the
+// bias is relative to c at the start of the key's aligned block of kPkRef keys.
 constexpr int kPkRef = 128;
+// P is carried as 2^15 P (see above): the exponent takes the 15, the results the inverse.
+constexpr float kPkLift = 15.0f, kPkUnlift = 1.0f / 32768.0f;
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) f16x8 lds_f16x8_t;
+
+// Round two floats to fp16 and back as one packed pair.
+__device__ __forceinline__ void round_f16_pair(float& a, float& b) {
+  f16x2 v = {(_Float16)a, (_Float16)b};
+  uint32_t w = __builtin_bit_cast(uint32_t, v);
+  asm volatile("" : "+v"(w));
+  v = __builtin_bit_cast(f16x2, w);
+  a = (float)v[0];
+  b = (float)v[1];
+}
 
 template <int D, int KS>
 struct alignas(256) PkDqSmem {
@@ -411,9 +431,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
 void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
                       const bf16* __restrict__ V, const float* __restrict__ C,
                       const float* __restrict__ LSE, const bf16* __restrict__ dO,
-                      const float* __restrict__ delta, bf16* __restrict__ dQ,
-                      float* __restrict__ dcq, const PackedItem* __restrict__ plan, int H, int Hkv,
-                      int N, float scale, float scale_log2) {
+                      float* __restrict__ delta, bf16* __restrict__ dQ,
+                      const PackedItem* __restrict__ plan, int H, int Hkv, int N, float scale,
+                      float scale_log2) {
   constexpr int TILE = kPkBN * D;
   constexpr int NDMA = TILE * 2 / 1024 / kPkWaves;
   __shared__ __attribute__((aligned(256))) PkDqSmem<D, KS> smem[KS];
@@ -489,7 +509,8 @@ void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   auto store_c = [&](int kt, auto bufc) {
     constexpr int B = decltype(bufc)::value;
     if (wave == 0) {
-      sm.c[B][lane] = kt * kPkBN + lane < L ? (craw - crefreg) * kLog2e : INFINITY;
+      sm.c[B][lane] =
+          kt * kPkBN + lane < L ? __builtin_fmaf(craw - crefreg, kLog2e, -kPkLift) : INFINITY;
       if (lane == 0) sm.cref[B] = crefreg;
     }
   };
@@ -555,7 +576,7 @@ void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
         }
       }
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) round_bf16_pair(pv[r], pv[r + 1]);
+      for (int r = 0; r < 16; r += 2) round_f16_pair(pv[r], pv[r + 1]);
       float dsv[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -634,7 +655,8 @@ void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
     }
   }
 
-  const float dcq_tot = wave_sum_pair(dcq_part);
+  const float dcq_tot = wave_sum_pair(dcq_part) * kPkUnlift;
+  const float f = scale * kPkUnlift;
   if (q_valid) {
     bf16* out = dQ + (at.row + qi) * D;
 #pragma unroll
@@ -643,10 +665,10 @@ void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
       for (int g = 0; g < 4; ++g) {
         bf16x4 w;
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) w[jj] = to_bf16(dqacc[db][4 * g + jj] * scale);
+        for (int jj = 0; jj < 4; ++jj) w[jj] = to_bf16(dqacc[db][4 * g + jj] * f);
         *reinterpret_cast<bf16x4*>(out + db * 32 + 8 * g + 4 * h) = w;
       }
-    if (h == 0) dcq[at.row + qi] = dcq_tot;
+    if (h == 0) delta[at.row + qi] = dlt + dcq_tot;
   }
 }
 
@@ -665,7 +687,7 @@ template <int D, int BM>
 struct PkKvSmem {
   bf16 q[3][BM * D];
   bf16 g[3][BM * D];
-  bf16x8 p[3][kPkPairs][BM / 16][64];
+  f16x8 p[3][kPkPairs][BM / 16][64];
   float bq[3][BM];      // ((c_i - c_ref) - LSE_i) / s of each query row
   float dl[3][BM];      // Delta_i
   float raw[2][3][64];  // c_i, LSE_i, Delta_i as loaded, two tiles ahead
@@ -782,7 +804,7 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   // c at k0 of the head that the converted tiles belong to (wave 0), of the head that the P
   // waves work on, and the key's term (c_j - c_k0) log2(e) of that head
   float conv_ck0 = C[row_of(0) + k0];
-  float ck2 = k_valid ? (C[row_of(0) + kj] - conv_ck0) * kLog2e : INFINITY;
+  float ck2 = k_valid ? __builtin_fmaf(C[row_of(0) + kj] - conv_ck0, kLog2e, -kPkLift) : INFINITY;
   float next_ckj = 0.0f, next_ck0 = 0.0f;
   auto convert_stats = [&](Turn x, int rb, auto bufc) {
     constexpr int B = decltype(bufc)::value;
@@ -845,7 +867,10 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
       static_for<2>([&](auto cc) {
         constexpr int ch = decltype(cc)::value;
         const bf16x8 pb = pack8(&pv[8 * ch]);
-        *(lds_bf16x8_t*)(p_at + B * kPBuf + (2 * qb + ch) * 1024) = pb;
+        f16x8 ph;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ph[i] = (_Float16)pv[8 * ch + i];
+        *(lds_f16x8_t*)(p_at + B * kPBuf + (2 * qb + ch) * 1024) = ph;
         lds_wait<1>(tr);  // the store may stay in flight
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
@@ -871,14 +896,14 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
       read_tr(bufc, std::integral_constant<int, 2 * qb>(), tr);
       static_for<2>([&](auto cc) {
         constexpr int ch = decltype(cc)::value;
-        const bf16x8 pb = *(const lds_bf16x8_t*)(p_at + B * kPBuf + (2 * qb + ch) * 1024);
+        const f16x8 ph = *(const lds_f16x8_t*)(p_at + B * kPBuf + (2 * qb + ch) * 1024);
         float dsv[8];
 #pragma unroll
         for (int g2 = 0; g2 < 2; ++g2) {
           const f32x4 dl4 = *(const lds_f32x4_t*)(row_at + kDlOff + 4 * (B * BM + qb * 32 + 8 * (2 * ch + g2)));
 #pragma unroll
           for (int jj = 0; jj < 4; ++jj) {
-            dsv[4 * g2 + jj] = to_f32(pb[4 * g2 + jj]) * (pacc[8 * ch + 4 * g2 + jj] - dl4[jj]);
+            dsv[4 * g2 + jj] = (float)ph[4 * g2 + jj] * (pacc[8 * ch + 4 * g2 + jj] - dl4[jj]);
             dck_part += dsv[4 * g2 + jj];
           }
         }
@@ -903,7 +928,7 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
     __syncthreads();  // tile `it` and P of tile it - 1 are in LDS
     // a new head: its c at the keys (loaded during the last step of the head before)
     if (pwave && it > 0 && it < total && cur.t == 0)
-      ck2 = k_valid ? (next_ckj - next_ck0) * kLog2e : INFINITY;
+      ck2 = k_valid ? __builtin_fmaf(next_ckj - next_ck0, kLog2e, -kPkLift) : INFINITY;
     if (it + 1 < total) issue_tile(ahead, std::integral_constant<int, BN>());
     if (it + 2 < total) issue_stats(ahead2, it & 1);
     if (pwave && it + 1 < total && ahead.t == 0) {
@@ -920,7 +945,7 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
     } else if (it >= 1 && it <= total) {
       if (t_first + prev.t >= t_diag) g_tile(std::integral_constant<int, BP>());
       if (prev.t + 1 == nt) {  // the head ends
-        const float tot = wave_sum_pair(dck_part);
+        const float tot = wave_sum_pair(dck_part) * kPkUnlift;
         if (k_valid && h == 0) dck[row_of(prev.g) + kj] = -tot;
         dck_part = 0.0f;
       }
@@ -946,7 +971,7 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
     step(it + 2, std::integral_constant<int, 2>());
   }
 
-  const float f = pwave ? 1.0f : scale;
+  const float f = (pwave ? 1.0f : scale) * kPkUnlift;
   if (splits > 1) {
     // partial dK and dV of these heads: [group][dK, dV][Hkv][N][D]
     if (k_valid) {
@@ -1055,7 +1080,7 @@ hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const 
 
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
                              const void* o, const float* lse, const void* d_o, void* dq, void* dk,
-                             void* dv, float* delta, float* dcq, float* dck, float* part,
+                             void* dv, float* delta, float* dck, float* part,
                              const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s) {
   hipError_t e = launch_bwd_delta(true, o, d_o, delta, H, N, d, s);
@@ -1071,14 +1096,14 @@ hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const 
   auto qs = [&](auto kernel, int groups) {
     hipLaunchKernelGGL(kernel, dim3(items * H), dim3(kPkThreads * groups), 0, s, (const bf16*)q,
                        (const bf16*)k, (const bf16*)v, c, lse, (const bf16*)d_o, delta, (bf16*)dq,
-                       dcq, (const PackedItem*)plan, H, Hkv, N, scale, scale * kLog2e);
+                       (const PackedItem*)plan, H, Hkv, N, scale, scale * kLog2e);
   };
   if (d == 128) {
-    kv(packed_dkdv_kernel<128, 64>);
     qs(packed_dq_kernel<128, 1>, 1);
+    kv(packed_dkdv_kernel<128, 64>);
   } else {
-    kv(packed_dkdv_kernel<64, 32>);
     qs(packed_dq_kernel<64, 1>, 1);
+    kv(packed_dkdv_kernel<64, 32>);
   }
   if (splits > 1) return launch_packed_head_sum(true, part, cu, dk, dv, B, Hkv, N, d, splits, s);
   return hipGetLastError();

@@ -1007,7 +1007,7 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
   float *dcq = delta + row, *dck = dcq + row, *part = dck + row;
   hipError_t e;
   if (dtype == FOX_DTYPE_BF16)
-    e = fox::launch_packed_bwd(q, k, v, c, o, lse, d_o, dq, dk, dv, delta, dcq, dck, part, plan,
+    e = fox::launch_packed_bwd(q, k, v, c, o, lse, d_o, dq, dk, dv, delta, dck, part, plan,
                                cu_seqlens, B, H, H_kv, N, d, len, scale, stream);
   else
     e = fox::launch_packed_bwd_f32((const float*)q, (const float*)k, (const float*)v, c,
@@ -1015,7 +1015,8 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
                                    (float*)dv, delta, dcq, dck, part, plan, cu_seqlens, B, H,
                                    H_kv, N, d, len, scale, stream);
   if (e == hipSuccess)
-    e = fox::launch_packed_gate_grad(gate_dtype == FOX_DTYPE_BF16, dcq, dck, gate_logit,
+    e = fox::launch_packed_gate_grad(gate_dtype == FOX_DTYPE_BF16,
+                                     dtype == FOX_DTYPE_BF16 ? nullptr : dcq, dck, gate_logit,
                                      cu_seqlens, d_log_f, d_logit, B, H, N, stream);
   return launch_status(e);
 }

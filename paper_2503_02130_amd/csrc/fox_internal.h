@@ -235,10 +235,10 @@ hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const 
 int packed_head_split(bool bf16, int H, int Hkv, int N, int d, int max_len);
 hipError_t launch_packed_head_sum(bool bf16, const float* part, const int* cu, void* dk, void* dv,
                                   int B, int Hkv, int N, int d, int splits, hipStream_t s);
-// dq, dk, dv, dc_q and dc_k (delta: [H, N] scratch)
+// dq, dk, dv and dc_k (delta: [H, N] scratch); in bf16 dc_q is 0, in fp32 it is given too
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
                              const void* o, const float* lse, const void* d_o, void* dq, void* dk,
-                             void* dv, float* delta, float* dcq, float* dck, float* part,
+                             void* dv, float* delta, float* dck, float* part,
                              const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s);
 hipError_t launch_packed_fwd_f32(const float* q, const float* k, const float* v, const float* c,

@@ -8,7 +8,7 @@
 //   prefix    c = the running sum of log sigmoid(logit) within each sequence, one workgroup
 //             per (head, sequence).
 //   gradient  d(logit)_l = sigmoid(-logit_l) sum_{i >= l} (dc_q_i + dc_k_i), the same from the
-//             sequence's end.
+//             sequence's end (without dc_q where it is 0).
 //
 // The scans run in 64 bits and round once: c of a long sequence is thousands with
 // differences of neighbours that matter, and fp32 sums of it are several units off.  They
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
       x[e] = 0.0f;
       if (p0 + e < L) {
         const size_t at = base + (GRAD ? L - 1 - p0 - e : p0 + e);
-        if constexpr (GRAD) x[e] = dcq[at] + dck[at];
+        if constexpr (GRAD) x[e] = dcq ? dcq[at] + dck[at] : dck[at];
         else x[e] = log_sigmoid(gate_at(logit, at));
       }
     }

@@ -13,7 +13,7 @@ def reference(q, k, v, logit, c32, cu, scale, d_o=None):
     {name: (value, bound)} for o, lse and, with d_o, dq, dk, dv, d_log_f, d_logit.
 
     c32 is the prefix sum that the kernels were given.  With e_p the relative error of a weight
-    (its rounding to bf16, if any, and the fp32 error of its exponent), a sum of w_j x_j is off
+    (its rounding, if any, and the fp32 error of its exponent), a sum of w_j x_j is off
     by at most sum |w_j x_j| (e_p + its fp32 summation), and a stored value by half a step
     more.  Delta comes from the stored O, so it is off by the products of |dO| and O's bound;
     dS = P (dP - Delta) by e_p of itself and P times Delta's error (and for the products once
