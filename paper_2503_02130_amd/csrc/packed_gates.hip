@@ -62,42 +62,78 @@ __global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict_
     for (long long i = total + lane; i < n_items; i += 64) items[i] = PackedItem{0, 0, 0, -1};
 }
 
-template <typename T>
-__device__ __forceinline__ float gate_at(const T* p, size_t i) {
-  return (float)p[i];
+// exp(a) on the transcendental unit: the product with log2(e) in two parts, so that large a keep
+// their digits.
+__device__ __forceinline__ float exp_short(float a) {
+  const float y = a * kLog2e;
+  const float lo = __builtin_fmaf(a, kLog2e, -y) + a * 1.9259629e-8f;  // log2(e) - float(log2(e))
+  const float e = exp2_fast(y);
+  return __builtin_fmaf(e, lo * kLn2, e);
+}
+// log sigmoid(x) = min(x, 0) - log1p(t), t = exp(-|x|), to a few units of the last place:
+// log1p(t) = log(u) t / (u - 1) with u = 1 + t rounded (t where u = 1), which cancels the
+// rounding of u.  A third of the instructions of expf and log1pf, which bound the scan of a
+// long row by one workgroup.
+__device__ __forceinline__ float log_sigmoid_short(float x) {
+  const float t = exp_short(-fabsf(x));
+  const float u = 1.0f + t, d = u - 1.0f;
+  const float l = d == 0.0f ? t : __builtin_amdgcn_logf(u) * kLn2 * t * __builtin_amdgcn_rcpf(d);
+  return fminf(x, 0.0f) - l;
+}
+// sigmoid(-x) = 1 / (1 + exp(x)), by the side that does not overflow
+__device__ __forceinline__ float sigmoid_neg_short(float x) {
+  const float t = exp_short(-fabsf(x));
+  return (x > 0.0f ? t : 1.0f) * __builtin_amdgcn_rcpf(1.0f + t);
 }
 
-// GRAD false: out = c from logits a; true: out = d(logit) from a = dc_q, b = dc_k, logits g,
-// and d(log f) if aux.
+// GRAD false: c from the logits; true: d(logit) from dc_q (may be NULL) and dc_k, and d(log f)
+// if aux.  Rows move between memory and LDS one lane beside the other; a thread scans eight
+// consecutive ones from there.
 template <bool GRAD, typename T>
 __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
     const float* __restrict__ dcq, const float* __restrict__ dck, const T* __restrict__ logit,
     const int* __restrict__ cu, float* __restrict__ c, float* __restrict__ aux,
     T* __restrict__ d_logit, int B, int H, int N) {
+  __shared__ __attribute__((aligned(16))) float row[kPScanSegment];
   __shared__ double wave_total[kPScanThreads / 64];
   const int b = (int)(blockIdx.x / H), h = (int)(blockIdx.x % H);
   int start, L;
   packed_range(cu, b, N, start, L);
+  // the sequence's rows, addressed by 32-bit offsets
   const size_t base = (size_t)h * N + start;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  logit += base;
+  if constexpr (GRAD) {
+    dck += base;
+    d_logit += base;
+    if (dcq) dcq += base;
+    if (aux) aux += base;
+  } else {
+    c += base;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   double carry = 0.0;
   for (int seg = 0; seg < L; seg += kPScanSegment) {
-    const int p0 = seg + threadIdx.x * kPScanPer;
-    // element e of the thread, in scan order, lies at row p0 + e, or L - 1 - p0 - e from the end
-    float x[kPScanPer];
+    const int m = min(kPScanSegment, L - seg);  // rows of this segment
+    // element p of the scan lies at row p, or L - 1 - p from the end
+    auto at = [&](int p) { return (unsigned)(GRAD ? L - 1 - p : p); };
 #pragma unroll
     for (int e = 0; e < kPScanPer; ++e) {
-      x[e] = 0.0f;
-      if (p0 + e < L) {
-        const size_t at = base + (GRAD ? L - 1 - p0 - e : p0 + e);
-        if constexpr (GRAD) x[e] = dcq ? dcq[at] + dck[at] : dck[at];
-        else x[e] = log_sigmoid(gate_at(logit, at));
+      const int i = e * kPScanThreads + tid;
+      float x = 0.0f;
+      if (i < m) {
+        const unsigned g = at(seg + i);
+        if constexpr (GRAD) x = dcq ? dcq[g] + dck[g] : dck[g];
+        else x = log_sigmoid_short((float)logit[g]);
       }
+      row[i] = x;
     }
+    __syncthreads();
+    f32x4* mine = reinterpret_cast<f32x4*>(row) + 2 * tid;
+    const f32x4 x0 = mine[0], x1 = mine[1];
     double run[kPScanPer], sum = 0.0;
 #pragma unroll
     for (int e = 0; e < kPScanPer; ++e) {
-      sum += x[e];
+      sum += e < 4 ? x0[e & 3] : x1[e & 3];
       run[e] = sum;
     }
     double incl = sum;
@@ -114,19 +150,30 @@ __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
       if (w < wave) prior += wave_total[w];
       carry += wave_total[w];
     }
+    f32x4 y0, y1;
 #pragma unroll
-    for (int e = 0; e < kPScanPer; ++e)
-      if (p0 + e < L) {
-        const size_t at = base + (GRAD ? L - 1 - p0 - e : p0 + e);
-        const float y = (float)(prior + run[e]);
+    for (int e = 0; e < 4; ++e) {
+      y0[e] = (float)(prior + run[e]);
+      y1[e] = (float)(prior + run[4 + e]);
+    }
+    mine[0] = y0;
+    mine[1] = y1;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kPScanPer; ++e) {
+      const int i = e * kPScanThreads + tid;
+      if (i < m) {
+        const unsigned g = at(seg + i);
+        const float y = row[i];
         if constexpr (GRAD) {
-          if (aux) aux[at] = y;
-          d_logit[at] = (T)(y / (1.0f + expf(gate_at(logit, at))));
+          if (aux) aux[g] = y;
+          d_logit[g] = (T)(y * sigmoid_neg_short((float)logit[g]));
         } else {
-          c[at] = y;
+          c[g] = y;
         }
       }
-    __syncthreads();
+    }
+    __syncthreads();  // the next segment writes the rows again
   }
 }
 
