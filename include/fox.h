@@ -526,19 +526,21 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  *   cu_seqlens     [B+1] int32, on the device: sequence b is rows cu_seqlens[b] ..
  *                  cu_seqlens[b+1] - 1; the first is 0, the last at most N, none is smaller
  *                  than the one before (a sequence may be empty).  Rows behind the last
- *                  sequence are neither read nor written, except by fox_packed_zero_behind.
+ *                  sequence are not read, and not written except to set them to zero.
  *   N * H and the rows of a head in bytes must be below 2^31.
  *
  * fox_packed_plan: the list of 128-row blocks that the attention calls walk, the heaviest
  *   first, into a device buffer of fox_packed_plan_bytes(); made once for a batch and used by
- *   every layer's forward and backward.
+ *   every layer's forward and backward.  With n tensors it does for them what
+ *   fox_packed_zero_behind does, in the same launch (n = 0: tensors may be NULL).
  * fox_gate_prefix_packed: c, the running sum of log sigmoid(gate_logit) within each sequence
  *   (summed in 64 bits, rounded once).
  * fox_attn_fwd_packed: O and LSE of each sequence as fox_attn_fwd's.  max_len: the longest
  *   sequence, if known, else 0 (N): it decides how the work is split, not what is computed.
  * fox_attn_bwd_packed: the gradients of sum(O o dO): dq, dk, dv (dk, dv summed over the query
  *   heads of a key head) and d_logit in gate_dtype, the gradient of the gate logits; d_log_f
- *   [H,N] fp32, that of log f, may be NULL.  workspace: at least
+ *   [H,N] fp32, that of log f, may be NULL.  With zero_behind not 0 the gradients' rows
+ *   behind the last sequence are set to zero.  workspace: at least
  *   fox_attn_bwd_packed_workspace_bytes() for the same max_len.
  * fox_packed_zero_behind: writes zeros to the rows behind the last sequence of n (at most 8)
  *   tensors [heads, N, row_bytes] on the device; row_bytes even.
@@ -551,7 +553,7 @@ typedef struct {
 
 size_t fox_packed_plan_bytes(int B, int N);
 fox_status_t fox_packed_plan(const int* cu_seqlens, int B, int N, void* plan, size_t plan_bytes,
-                    hipStream_t stream);
+                    const fox_packed_rows_t* tensors, int n, hipStream_t stream);
 fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_logit,
                            const int* cu_seqlens, float* c, int B, int H, int N,
                            hipStream_t stream);
@@ -564,8 +566,9 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
                         const float* c, const void* o, const float* lse, const void* d_o,
                         fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
                         const void* plan, void* dq, void* dk, void* dv, void* d_logit,
-                        float* d_log_f, void* workspace, size_t workspace_bytes, int B, int H,
-                        int H_kv, int N, int d, int max_len, float scale, hipStream_t stream);
+                        float* d_log_f, int zero_behind, void* workspace,
+                        size_t workspace_bytes, int B, int H, int H_kv, int N, int d,
+                        int max_len, float scale, hipStream_t stream);
 fox_status_t fox_packed_zero_behind(const fox_packed_rows_t* tensors, int n, const int* cu_seqlens,
                            int B, int N, hipStream_t stream);
 

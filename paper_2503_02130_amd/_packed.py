@@ -53,7 +53,7 @@ def fox_packed_plan(cu_seqlens: torch.Tensor, N: int) -> torch.Tensor:
     lib = load()
     places = _plan_places(B, N)
     plan = torch.empty((places * 4,), device=dev, dtype=torch.int32)
-    st = _call(lib.fox_packed_plan, dev, _ptr(cu_seqlens), B, N, _ptr(plan), 16 * places)
+    st = _call(lib.fox_packed_plan, dev, _ptr(cu_seqlens), B, N, _ptr(plan), 16 * places, None, 0)
     _raise(st, "fox_packed_plan")
     return plan
 
@@ -155,7 +155,7 @@ def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
     s = default_scale(d) if scale is None else float(scale)
     st = _call(lib.fox_attn_bwd_packed, dev, _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(o),
                _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), _ptr(cu_seqlens), _ptr(plan),
-               _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_logit), _ptr(d_log_f), _ptr(workspace),
+               _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_logit), _ptr(d_log_f), 0, _ptr(workspace),
                nbytes, B, H, Hkv, N, d, max_len, s)
     _raise(st, "fox_attn_bwd_packed")
     return dq, dk, dv, d_logit
@@ -187,22 +187,22 @@ def _step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
     _need(gate_logit, "gate_logit", (H, N), gdt, dev)
     B = _check_cu(cu_seqlens, dev)
     lib, cu = load(), _ptr(cu_seqlens)
+    c, lse = (torch.empty((H, N), device=dev, dtype=torch.float32) for _ in range(2))
+    o = torch.empty_like(q)
+    row = _RowsStruct(_ptr(o), H, d * o.element_size())
     if plan is None:
         places = _plan_places(B, N)
         plan = torch.empty((places * 4,), device=dev, dtype=torch.int32)
-        _raise(_call(lib.fox_packed_plan, dev, cu, B, N, _ptr(plan), 16 * places),
-               "fox_packed_plan")
+        _raise(_call(lib.fox_packed_plan, dev, cu, B, N, _ptr(plan), 16 * places,
+                     ctypes.addressof(row), 1), "fox_packed_plan")
     else:
         _check_plan(plan, B, N, dev)
-    c, lse = (torch.empty((H, N), device=dev, dtype=torch.float32) for _ in range(2))
-    o = torch.empty_like(q)
+        _raise(_call(lib.fox_packed_zero_behind, dev, ctypes.addressof(row), 1, cu, B, N),
+               "fox_packed_zero_behind")
     _raise(_call(lib.fox_gate_prefix_packed, dev, _DT[gdt], _ptr(gate_logit), cu, _ptr(c), B, H, N),
            "fox_gate_prefix_packed")
     _raise(_call(lib.fox_attn_fwd_packed, dev, dt, _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(plan),
                  _ptr(o), _ptr(lse), B, H, Hkv, N, d, max_len, scale), "fox_attn_fwd_packed")
-    row = _RowsStruct(_ptr(o), H, d * o.element_size())
-    _raise(_call(lib.fox_packed_zero_behind, dev, ctypes.addressof(row), 1, cu, B, N),
-           "fox_packed_zero_behind")
     return plan, c, o, lse
 
 
@@ -219,11 +219,6 @@ def _step_backward(saved, d_o, max_len, scale):
     ws = _workspace(nbytes, dev)
     _raise(_call(lib.fox_attn_bwd_packed, dev, _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c),
                  _ptr(o), _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), cu, _ptr(plan),
-                 *map(_ptr, grads), None, _ptr(ws), nbytes, B, H, Hkv, N, d, max_len, scale),
+                 *map(_ptr, grads), None, 1, _ptr(ws), nbytes, B, H, Hkv, N, d, max_len, scale),
            "fox_attn_bwd_packed")
-    e, ge = q.element_size(), gate_logit.element_size()
-    rows = (_RowsStruct * 4)((_ptr(grads[0]), H, d * e), (_ptr(grads[1]), Hkv, d * e),
-                             (_ptr(grads[2]), Hkv, d * e), (_ptr(grads[3]), H, ge))
-    _raise(_call(lib.fox_packed_zero_behind, dev, ctypes.addressof(rows), 4, cu, B, N),
-           "fox_packed_zero_behind")
     return grads

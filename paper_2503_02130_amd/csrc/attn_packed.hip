@@ -19,7 +19,8 @@
 //     sums are added up afterwards (packed_head_split).  dc^k, which belongs to a query head,
 //     is written as each head ends.
 //   * The row sum l adds the unrounded fp32 P, so that LSE is an fp32 quantity to its last
-//     digits.  The backward forms dS from P rounded to fp16 (2^-12 of it; carried as 2^15 P,
+//     digits.  The dQ kernel forms Delta itself from the rows of O and dO that it owns.  The
+//     backward forms dS from P rounded to fp16 (2^-12 of it; carried as 2^15 P,
 //     which fp16 holds to full precision down to 2^-29) and dc^k adds the unrounded fp32 dS.
 //   * c_i shifts a whole softmax row, so dc^q = rowsum(dS) is 0; what it comes out as is the
 //     error of Delta, formed from O as rounded to bf16.  The dQ kernel runs first and adds its
@@ -431,9 +432,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
 void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
                       const bf16* __restrict__ V, const float* __restrict__ C,
                       const float* __restrict__ LSE, const bf16* __restrict__ dO,
-                      float* __restrict__ delta, bf16* __restrict__ dQ,
-                      const PackedItem* __restrict__ plan, int H, int Hkv, int N, float scale,
-                      float scale_log2) {
+                      const bf16* __restrict__ O, float* __restrict__ delta,
+                      bf16* __restrict__ dQ, const PackedItem* __restrict__ plan, int H, int Hkv,
+                      int N, float scale, float scale_log2) {
   constexpr int TILE = kPkBN * D;
   constexpr int NDMA = TILE * 2 / 1024 / kPkWaves;
   __shared__ __attribute__((aligned(256))) PkDqSmem<D, KS> smem[KS];
@@ -474,7 +475,17 @@ void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   }
   const float cq = q_valid ? c[qi] : 0.0f;
   const float lse_q = q_valid ? LSE[at.row + qi] : 0.0f;
-  const float dlt = q_valid ? delta[at.row + qi] : 0.0f;
+  // Delta_i = dO_i . O_i: a lane holds half of its row's dims, in the pieces of its operands
+  float dlt = 0.0f;
+  if (q_valid) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const bf16x8 ov = *reinterpret_cast<const bf16x8*>(O + (at.row + qi) * D + 16 * s + 8 * h);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dlt = __builtin_fmaf(to_f32(ov[e]), to_f32(dof[s][e]), dlt);
+    }
+  }
+  dlt = wave_sum_pair(dlt);
 
   f32x16 dqacc[D / 32];
 #pragma unroll
@@ -1064,6 +1075,28 @@ int packed_head_split(bool bf16_, int H, int Hkv, int N, int d, int max_len) {
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
+// Wave groups of a workgroup that share a row block's key tiles: more than one where the grid
+// is short and the longest row's chain of tiles decides the time, by the rules of the dense
+// kernels, whose tiles these are (attn_fwd.hip, attn_bwd.hip); the workgroups are counted as the
+// rows' blocks and the longest row as max_len.  Measured with H = 16, Hkv = 4 (us, one group /
+// split): one sequence of 3001, D = 128 62.4 / 50.6 forward; D = 64 45.1 / 38.6; one of 4000,
+// H = 12, D = 64 58.5 / 44.5.
+static long long row_blocks(int H, int N) {
+  return (long long)H * ((N + kPackedBlock - 1) / kPackedBlock);
+}
+static int packed_fwd_groups(int d, long long wgs, int max_len) {
+  const long long tiles = (max_len + kPkBN - 1) / kPkBN;
+  if (d == 64) {
+    if (wgs <= 512 && tiles >= 24 && 12 * tiles >= wgs) return 4;
+    return wgs <= 1024 && tiles >= 12 && 16 * tiles >= wgs ? 2 : 1;
+  }
+  return wgs <= 512 && tiles >= 16 && 16 * tiles >= wgs ? 2 : 1;
+}
+static bool packed_dq_split(long long wgs, int max_len) {
+  const long long tiles = (max_len + kPkBN - 1) / kPkBN;
+  return wgs <= 512 && tiles >= 8 && 24 * tiles >= wgs;
+}
+
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
                              float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s) {
@@ -1073,8 +1106,15 @@ hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const 
                        (const bf16*)k, (const bf16*)v, c, (bf16*)o, lse, (const PackedItem*)plan,
                        H, Hkv, N, scale * kLog2e);
   };
-  if (d == 128) run(packed_fwd_kernel<128, 1>, 1);
-  else run(packed_fwd_kernel<64, 1>, 1);
+  const int groups = packed_fwd_groups(d, row_blocks(H, N), max_len);
+  if (d == 128) {
+    if (groups == 1) run(packed_fwd_kernel<128, 1>, 1);
+    else run(packed_fwd_kernel<128, 2>, 2);
+  } else {
+    if (groups == 1) run(packed_fwd_kernel<64, 1>, 1);
+    else if (groups == 2) run(packed_fwd_kernel<64, 2>, 2);
+    else run(packed_fwd_kernel<64, 4>, 4);
+  }
   return hipGetLastError();
 }
 
@@ -1083,8 +1123,6 @@ hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const 
                              void* dv, float* delta, float* dck, float* part,
                              const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s) {
-  hipError_t e = launch_bwd_delta(true, o, d_o, delta, H, N, d, s);
-  if (e != hipSuccess) return e;
   const unsigned items = (unsigned)packed_items(B, N);
   const int splits = packed_head_split(true, H, Hkv, N, d, max_len);
   auto kv = [&](auto kernel) {
@@ -1093,16 +1131,19 @@ hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const 
                        (bf16*)dv, dck, part, (const PackedItem*)plan, H, Hkv, splits, N, scale,
                        scale * kLog2e);
   };
+  const bool split = packed_dq_split(row_blocks(H, N), max_len);
   auto qs = [&](auto kernel, int groups) {
     hipLaunchKernelGGL(kernel, dim3(items * H), dim3(kPkThreads * groups), 0, s, (const bf16*)q,
-                       (const bf16*)k, (const bf16*)v, c, lse, (const bf16*)d_o, delta, (bf16*)dq,
-                       (const PackedItem*)plan, H, Hkv, N, scale, scale * kLog2e);
+                       (const bf16*)k, (const bf16*)v, c, lse, (const bf16*)d_o, (const bf16*)o, delta,
+                       (bf16*)dq, (const PackedItem*)plan, H, Hkv, N, scale, scale * kLog2e);
   };
   if (d == 128) {
-    qs(packed_dq_kernel<128, 1>, 1);
+    if (split) qs(packed_dq_kernel<128, kPkDqGroups<128>>, kPkDqGroups<128>);
+    else qs(packed_dq_kernel<128, 1>, 1);
     kv(packed_dkdv_kernel<128, 64>);
   } else {
-    qs(packed_dq_kernel<64, 1>, 1);
+    if (split) qs(packed_dq_kernel<64, kPkDqGroups<64>>, kPkDqGroups<64>);
+    else qs(packed_dq_kernel<64, 1>, 1);
     kv(packed_dkdv_kernel<64, 32>);
   }
   if (splits > 1) return launch_packed_head_sum(true, part, cu, dk, dv, B, Hkv, N, d, splits, s);

@@ -104,6 +104,19 @@ fox_status_t check_packed(int B, int H, int H_kv, int N) {
   return FOX_OK;
 }
 
+fox_status_t zero_rows(const fox_packed_rows_t* tensors, int n, fox::ZeroRows* x) {
+  if (n < 0 || n > fox::kZeroTensors) return FOX_ERR_SHAPE;
+  if (n > 0 && !tensors) return FOX_ERR_NULL;
+  for (int i = 0; i < n; ++i) {
+    if (!tensors[i].x) return FOX_ERR_NULL;
+    if (tensors[i].heads <= 0 || tensors[i].row_bytes <= 0 || tensors[i].row_bytes % 2)
+      return FOX_ERR_SHAPE;
+    if (!aligned16(tensors[i].x)) return FOX_ERR_ALIGN;
+    x[i] = fox::ZeroRows{tensors[i].x, tensors[i].heads, tensors[i].row_bytes};
+  }
+  return FOX_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -931,13 +944,16 @@ size_t fox_packed_plan_bytes(int B, int N) {
 }
 
 fox_status_t fox_packed_plan(const int* cu_seqlens, int B, int N, void* plan, size_t plan_bytes,
-                    hipStream_t stream) {
+                    const fox_packed_rows_t* tensors, int n, hipStream_t stream) {
   if (!cu_seqlens || !plan) return FOX_ERR_NULL;
   fox_status_t st = check_packed(B, 1, 1, N);
   if (st) return st;
   if (!all_aligned16({cu_seqlens, plan})) return FOX_ERR_ALIGN;
   if (plan_bytes < fox_packed_plan_bytes(B, N)) return FOX_ERR_WORKSPACE;
-  return launch_status(fox::launch_packed_plan(cu_seqlens, B, N, plan, stream));
+  fox::ZeroRows x[fox::kZeroTensors];
+  st = zero_rows(tensors, n, x);
+  if (st) return st;
+  return launch_status(fox::launch_packed_plan(cu_seqlens, B, N, plan, x, n, stream));
 }
 
 fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_logit,
@@ -984,8 +1000,9 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
                         const float* c, const void* o, const float* lse, const void* d_o,
                         fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
                         const void* plan, void* dq, void* dk, void* dv, void* d_logit,
-                        float* d_log_f, void* workspace, size_t workspace_bytes, int B, int H,
-                        int H_kv, int N, int d, int max_len, float scale, hipStream_t stream) {
+                        float* d_log_f, int zero_behind, void* workspace,
+                        size_t workspace_bytes, int B, int H, int H_kv, int N, int d,
+                        int max_len, float scale, hipStream_t stream) {
   if (!all_set({q, k, v, c, o, lse, d_o, gate_logit, cu_seqlens, plan, dq, dk, dv, d_logit}))
     return FOX_ERR_NULL;
   fox_status_t st = check_packed(B, H, H_kv, N);
@@ -1014,25 +1031,27 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
                                    (const float*)o, lse, (const float*)d_o, (float*)dq, (float*)dk,
                                    (float*)dv, delta, dcq, dck, part, plan, cu_seqlens, B, H,
                                    H_kv, N, d, len, scale, stream);
+  const int esz = dtype == FOX_DTYPE_BF16 ? 2 : 4;
+  const fox::ZeroRows zeros[] = {{dq, H, d * esz},
+                                 {dk, H_kv, d * esz},
+                                 {dv, H_kv, d * esz},
+                                 {d_logit, H, gate_dtype == FOX_DTYPE_BF16 ? 2 : 4},
+                                 {d_log_f, H, 4}};
   if (e == hipSuccess)
     e = fox::launch_packed_gate_grad(gate_dtype == FOX_DTYPE_BF16,
                                      dtype == FOX_DTYPE_BF16 ? nullptr : dcq, dck, gate_logit,
-                                     cu_seqlens, d_log_f, d_logit, B, H, N, stream);
+                                     cu_seqlens, d_log_f, d_logit, B, H, N, zeros,
+                                     !zero_behind ? 0 : d_log_f ? 5 : 4, stream);
   return launch_status(e);
 }
 
 fox_status_t fox_packed_zero_behind(const fox_packed_rows_t* tensors, int n, const int* cu_seqlens,
                            int B, int N, hipStream_t stream) {
-  if (!tensors || !cu_seqlens) return FOX_ERR_NULL;
-  if (n < 1 || n > fox::kZeroTensors || B <= 0 || N <= 0) return FOX_ERR_SHAPE;
+  if (!cu_seqlens) return FOX_ERR_NULL;
+  if (n < 1 || B <= 0 || N <= 0) return FOX_ERR_SHAPE;
   fox::ZeroRows x[fox::kZeroTensors];
-  for (int i = 0; i < n; ++i) {
-    if (!tensors[i].x) return FOX_ERR_NULL;
-    if (tensors[i].heads <= 0 || tensors[i].row_bytes <= 0 || tensors[i].row_bytes % 2)
-      return FOX_ERR_SHAPE;
-    if (!aligned16(tensors[i].x)) return FOX_ERR_ALIGN;
-    x[i] = fox::ZeroRows{tensors[i].x, tensors[i].heads, tensors[i].row_bytes};
-  }
+  fox_status_t st = zero_rows(tensors, n, x);
+  if (st) return st;
   return launch_status(fox::launch_packed_zero(x, n, cu_seqlens, B, N, stream));
 }
 

@@ -214,12 +214,7 @@ hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_l
 // Packed sequences (packed_gates.hip, attn_packed.hip; fp32 in attn_f32.hip): cu [B + 1], N rows.
 // The plan holds packed_items() places of 16 bytes.
 int packed_items(int B, int N);
-hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, hipStream_t s);
-hipError_t launch_packed_prefix(bool bf16, const void* logit, const int* cu, float* c, int B,
-                                int H, int N, hipStream_t s);
-hipError_t launch_packed_gate_grad(bool bf16, const float* dcq, const float* dck,
-                                   const void* logit, const int* cu, float* d_log_f,
-                                   void* d_logit, int B, int H, int N, hipStream_t s);
+// tensors [heads, N, row] whose rows behind the last sequence are set to zero
 struct ZeroRows {
   void* p;
   int heads, row_bytes;  // an even number of bytes
@@ -227,6 +222,14 @@ struct ZeroRows {
 constexpr int kZeroTensors = 8;
 hipError_t launch_packed_zero(const ZeroRows* x, int n, const int* cu, int B, int N,
                               hipStream_t s);
+hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, const ZeroRows* zeros,
+                              int n_zeros, hipStream_t s);
+hipError_t launch_packed_prefix(bool bf16, const void* logit, const int* cu, float* c, int B,
+                                int H, int N, hipStream_t s);
+hipError_t launch_packed_gate_grad(bool bf16, const float* dcq, const float* dck,
+                                   const void* logit, const int* cu, float* d_log_f,
+                                   void* d_logit, int B, int H, int N, const ZeroRows* zeros,
+                                   int n_zeros, hipStream_t s);
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
                              float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s);

@@ -31,9 +31,44 @@ __device__ __forceinline__ void packed_range(const int* __restrict__ cu, int b, 
   len = max(min(cu[b + 1], N) - start, 0);
 }
 
+// Zeros in the rows behind the last sequence of up to kZeroTensors tensors [heads, N, row], by
+// workgroup `group` of kZeroGroups.
+struct ZeroList {
+  ZeroRows x[kZeroTensors];
+  int n;
+};
+constexpr int kZeroGroups = 64;
+static ZeroList zero_list(const ZeroRows* x, int n) {
+  ZeroList list;
+  list.n = n;
+  for (int i = 0; i < n; ++i) list.x[i] = x[i];
+  return list;
+}
+__device__ __forceinline__ void zero_behind(const ZeroList& list, const int* __restrict__ cu, int B,
+                                            int N, int group) {
+  const int first = min(max(cu[B], 0), N);
+  if (first == N) return;
+  for (int i = 0; i < list.n; ++i) {
+    const ZeroRows z = list.x[i];
+    const long long per = (long long)(N - first) * (z.row_bytes / 2);  // 2 bytes divide any row
+    for (long long j = (long long)group * blockDim.x + threadIdx.x; j < per * z.heads;
+         j += (long long)kZeroGroups * blockDim.x) {
+      const long long h = j / per, at = j % per;
+      static_cast<uint16_t*>(z.p)[(h * N + first) * (z.row_bytes / 2) + at] = 0;
+    }
+  }
+}
+__global__ __launch_bounds__(256) void packed_zero_kernel(ZeroList list, const int* __restrict__ cu,
+                                                          int B, int N) {
+  zero_behind(list, cu, B, N, (int)blockIdx.x);
+}
+
 __global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict__ cu, int B, int N,
                                                           PackedItem* __restrict__ items,
-                                                          int n_items) {
+                                                          int n_items, int plan_groups,
+                                                          ZeroList zeros) {
+  if ((int)blockIdx.x >= plan_groups)
+    return zero_behind(zeros, cu, B, N, (int)blockIdx.x - plan_groups);
   const int lane = threadIdx.x & 63;
   const int m = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
   long long before = 0, total = 0;
@@ -93,7 +128,8 @@ template <bool GRAD, typename T>
 __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
     const float* __restrict__ dcq, const float* __restrict__ dck, const T* __restrict__ logit,
     const int* __restrict__ cu, float* __restrict__ c, float* __restrict__ aux,
-    T* __restrict__ d_logit, int B, int H, int N) {
+    T* __restrict__ d_logit, int B, int H, int N, ZeroList zeros) {
+  if (GRAD && (int)blockIdx.x >= B * H) return zero_behind(zeros, cu, B, N, (int)blockIdx.x - B * H);
   __shared__ __attribute__((aligned(16))) float row[kPScanSegment];
   __shared__ double wave_total[kPScanThreads / 64];
   const int b = (int)(blockIdx.x / H), h = (int)(blockIdx.x % H);
@@ -179,10 +215,12 @@ __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
 
 int packed_items(int B, int N) { return N / kPackedBlock + std::min(B, N); }
 
-hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, hipStream_t s) {
-  const int waves = (N + kPackedBlock - 1) / kPackedBlock;
-  hipLaunchKernelGGL(packed_plan_kernel, dim3((waves + 3) / 4), dim3(256), 0, s, cu, B, N,
-                     (PackedItem*)plan, packed_items(B, N));
+hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, const ZeroRows* zeros,
+                              int n_zeros, hipStream_t s) {
+  const int groups = ((N + kPackedBlock - 1) / kPackedBlock + 3) / 4;  // a wave per block number
+  hipLaunchKernelGGL(packed_plan_kernel, dim3(groups + (n_zeros ? kZeroGroups : 0)), dim3(256), 0, s,
+                     cu, B, N, (PackedItem*)plan, packed_items(B, N), groups,
+                     zero_list(zeros, n_zeros));
   return hipGetLastError();
 }
 
@@ -191,52 +229,33 @@ hipError_t launch_packed_prefix(bool bf16_, const void* logit, const int* cu, fl
   const dim3 grid((unsigned)B * (unsigned)H), block(kPScanThreads);
   if (bf16_)
     hipLaunchKernelGGL((packed_scan_kernel<false, bf16>), grid, block, 0, s, nullptr, nullptr,
-                       (const bf16*)logit, cu, c, nullptr, nullptr, B, H, N);
+                       (const bf16*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{});
   else
     hipLaunchKernelGGL((packed_scan_kernel<false, float>), grid, block, 0, s, nullptr, nullptr,
-                       (const float*)logit, cu, c, nullptr, nullptr, B, H, N);
+                       (const float*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{});
   return hipGetLastError();
 }
 
 hipError_t launch_packed_gate_grad(bool bf16_, const float* dcq, const float* dck,
                                    const void* logit, const int* cu, float* d_log_f,
-                                   void* d_logit, int B, int H, int N, hipStream_t s) {
-  const dim3 grid((unsigned)B * (unsigned)H), block(kPScanThreads);
+                                   void* d_logit, int B, int H, int N, const ZeroRows* zeros,
+                                   int n_zeros, hipStream_t s) {
+  const dim3 grid((unsigned)B * (unsigned)H + (n_zeros ? kZeroGroups : 0)), block(kPScanThreads);
   if (bf16_)
     hipLaunchKernelGGL((packed_scan_kernel<true, bf16>), grid, block, 0, s, dcq, dck,
-                       (const bf16*)logit, cu, nullptr, d_log_f, (bf16*)d_logit, B, H, N);
+                       (const bf16*)logit, cu, nullptr, d_log_f, (bf16*)d_logit, B, H, N,
+                       zero_list(zeros, n_zeros));
   else
     hipLaunchKernelGGL((packed_scan_kernel<true, float>), grid, block, 0, s, dcq, dck,
-                       (const float*)logit, cu, nullptr, d_log_f, (float*)d_logit, B, H, N);
+                       (const float*)logit, cu, nullptr, d_log_f, (float*)d_logit, B, H, N,
+                       zero_list(zeros, n_zeros));
   return hipGetLastError();
-}
-
-// Zeros in the rows behind the last sequence of up to kZeroTensors tensors [heads, N, row].
-struct ZeroList {
-  ZeroRows x[kZeroTensors];
-  int n;
-};
-__global__ __launch_bounds__(256) void packed_zero_kernel(ZeroList list, const int* __restrict__ cu,
-                                                          int B, int N) {
-  const int first = min(max(cu[B], 0), N);
-  for (int i = 0; i < list.n; ++i) {
-    // every tensor in its own type's pieces: 2 bytes divide any row
-    const ZeroRows z = list.x[i];
-    const long long per = (long long)(N - first) * (z.row_bytes / 2);
-    for (long long j = (long long)blockIdx.x * 256 + threadIdx.x; j < per * z.heads;
-         j += (long long)gridDim.x * 256) {
-      const long long h = j / per, at = j % per;
-      static_cast<uint16_t*>(z.p)[(h * N + first) * (z.row_bytes / 2) + at] = 0;
-    }
-  }
 }
 
 hipError_t launch_packed_zero(const ZeroRows* x, int n, const int* cu, int B, int N,
                               hipStream_t s) {
-  ZeroList list;
-  list.n = n;
-  for (int i = 0; i < n; ++i) list.x[i] = x[i];
-  hipLaunchKernelGGL(packed_zero_kernel, dim3(256), dim3(256), 0, s, list, cu, B, N);
+  hipLaunchKernelGGL(packed_zero_kernel, dim3(kZeroGroups), dim3(256), 0, s, zero_list(x, n), cu, B,
+                     N);
   return hipGetLastError();
 }
 
