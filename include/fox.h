@@ -525,14 +525,16 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  *   gate logits    [H,N] fp32 or bf16 (gate_dtype)     c, lse [H,N] fp32
  *   cu_seqlens     [B+1] int32, on the device: sequence b is rows cu_seqlens[b] ..
  *                  cu_seqlens[b+1] - 1; the first is 0, the last at most N, none is smaller
- *                  than the one before (a sequence may be empty).  Rows behind the last
- *                  sequence are not read, and not written except to set them to zero.
+ *                  than the one before (a sequence may be empty).  What rows behind the last
+ *                  sequence hold does not matter; they are not written except to set them
+ *                  to zero.
  *   N * H and the rows of a head in bytes must be below 2^31.
  *
  * fox_packed_plan: the list of 128-row blocks that the attention calls walk, the heaviest
- *   first, into a device buffer of fox_packed_plan_bytes(); made once for a batch and used by
- *   every layer's forward and backward.  With n tensors it does for them what
- *   fox_packed_zero_behind does, in the same launch (n = 0: tensors may be NULL).
+ *   first, into a device buffer of fox_packed_plan_bytes(); made once for a batch (its
+ *   cu_seqlens, B and N) and used by every layer's forward and backward.  With n tensors it
+ *   does for them what fox_packed_zero_behind does, in the same launch (n = 0: tensors may be
+ *   NULL).  Blocks of a list that do not lie within a call's N rows are skipped.
  * fox_gate_prefix_packed: c, the running sum of log sigmoid(gate_logit) within each sequence
  *   (summed in 64 bits, rounded once).
  * fox_attn_fwd_packed: O and LSE of each sequence as fox_attn_fwd's.  max_len: the longest
@@ -612,8 +614,8 @@ typedef struct {
 } fox_cache_t;
 
 /*
- * fox_cache_append: writes n new tokens of each sequence (1 <= n <= 64) behind its seq_len[b]
- *   cached ones.
+ * fox_cache_append: writes n new tokens of each sequence (1 <= n <= 64, B H n at most 2^22)
+ *   behind its seq_len[b] cached ones.
  *     k, v        [B,H_kv,n,d] dtype in   (fp32 is rounded once, to the cache's type)
  *     gate_logit  [B,H,n]      fp32 in
  *     parent      [B,n] int32  in   the new token that a new token follows, less than its own
@@ -624,7 +626,7 @@ typedef struct {
  * fox_cache_append_packed: writes whole prompts, packed as for fox_attn_fwd_packed, behind
  *   the seq_len[b] cached tokens (NULL: into empty caches).  c [H,N] fp32 comes from
  *   fox_gate_prefix_packed; a cached sequence's last c is added to it.
- *     k, v [H_kv,N,d] dtype in;  cu_seqlens [B+1] int32 in
+ *     k, v [H_kv,N,d] dtype in;  cu_seqlens [B+1] int32 in;  N (H + H_kv d / 8) below 2^32
  * fox_cache_keep: moves token seq_len[b] + index[b,j] to place seq_len[b] + j, for j below
  *   n_keep[b] (at most n, n <= 64; indexes 0..63): the accepted path of a tree of drafts.
  *   Everything is read before it is written, so any indexes may be given.  The caller then
@@ -632,7 +634,8 @@ typedef struct {
  *     index [B,n] int32 in;  n_keep [B] int32 in
  * fox_cache_read: positions start[b] + t, t < T, below seq_len[b], as dtype: k, v
  *   [B,H_kv,T,d], c [B,H,T] fp32 (may be NULL); start may be NULL (0).  Other rows of the
- *   outputs are left as they were, or set to zero if zero_others is not 0.
+ *   outputs are left as they were, or set to zero if zero_others is not 0.  B T in place of
+ *   N: the same bound.
  */
 fox_status_t fox_cache_append(const fox_cache_t* cache, fox_dtype_t dtype, const void* k, const void* v,
                      const float* gate_logit, const int* seq_len, const int* parent,
@@ -647,7 +650,7 @@ fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const i
                    hipStream_t stream);
 
 /*
- * Attention of n new tokens of each sequence (1 <= n <= 64) over the cache that holds them
+ * Attention of n new tokens of each sequence (1 <= n <= 64, B H n at most 2^22) over the cache that holds them
  * already, at places seq_len[b] .. seq_len[b] + n - 1 (fox_cache_append): each attends to the
  * seq_len[b] tokens before them and, among the new ones, to its ancestors and itself.  n = 1
  * is a decode step.
@@ -656,12 +659,14 @@ fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const i
  *   o       [B,H,n,d] bf16 out     lse [B,H,n] fp32 out, as fox_attn_fwd's
  *           rows of tokens that a sequence does not have (n_new) are left as they were; a
  *           token whose own place is not in the cache gets o = 0 and lse = -inf
- *   max_len the most tokens that a sequence has, new ones included: the keys are split for
- *           it.  Longer sequences are right too, only slower.  0: max_pages * page.
+ *   max_len the most tokens that a sequence has, new ones included: it bounds the parts that
+ *           the keys are split into, and the workspace.  Longer sequences are right too, only
+ *           slower.  0: max_pages * page.
  *   workspace  at least fox_attn_cache_workspace_bytes() for the same n and max_len (which
  *           may be 0: then workspace may be NULL)
- * k and v of the tokens in the cache must be finite.  The order of the sums depends on the
- * shape and on max_len, not on what other sequences hold.
+ * k and v of the tokens in the cache must be finite.  A sequence's keys are split into parts by
+ * the shape, max_len and the lengths of all sequences, so its results in another batch agree to
+ * rounding; the same call gives the same bits.
  */
 size_t fox_attn_cache_workspace_bytes(const fox_cache_t* cache, int n, int max_len);
 fox_status_t fox_attn_cache(const fox_cache_t* cache, const void* q, const int* seq_len,

@@ -180,7 +180,8 @@ def fox_attn_cache(q: torch.Tensor, cache: PagedCache, seq_len: torch.Tensor,
     """O [B,H,n,d] bf16 and LSE [B,H,n] fp32 of the n <= 64 newest tokens of each sequence
     (at places seq_len[b] .., written by fox_cache_append with the same parent and n_new)
     over the cache.  n = 1 is a decode step.  max_len: the most tokens a sequence has, new
-    ones included (0: what the page table holds); it sets how the keys are split."""
+    ones included (0: what the page table holds); it bounds the parts that the keys are split
+    into, and the workspace."""
     B, H, n, d = q.shape
     dev = cache.device
     _need(q, "q", (cache.B, cache.H, n, cache.d), torch.bfloat16, dev)

@@ -188,7 +188,7 @@ template <bool PK>
 __device__ __forceinline__ bool f32_query_place(long long blk, int n_blk, int BH, int L,
                                                 const F32Packed& pk, F32Place& p) {
   if constexpr (PK) {
-    const PackedItem it = pk.plan[blk / (4 * pk.H)];
+    const PackedItem it = packed_item(pk.plan, (size_t)(blk / (4 * pk.H)), pk.N);
     const int i = (int)(blk % (4 * pk.H));
     p.bh = packed_head(i % pk.H, pk.Hkv, pk.H / pk.Hkv);
     p.mb = 4 * it.block + 3 - i / pk.H;
@@ -498,7 +498,7 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
     if constexpr (PK) {
       // an item's block m, as keys, is block n - 1 - m of the sequence's n
       const int per = pk.Hkv * pk.splits;
-      const PackedItem it = pk.plan[blk / (4 * per)];
+      const PackedItem it = packed_item(pk.plan, (size_t)(blk / (4 * per)), pk.N);
       const int i = (int)(blk % (4 * per)), hk = i % pk.Hkv;
       hg = i / pk.Hkv % pk.splits;
       L = it.len;
@@ -522,71 +522,71 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
 
     // the query heads of this key head (dense: one)
     for (int g = 0; g < G; ++g, head += PK ? pk.N : 0) {
-    const GateRow<FIXED> gr(gate, bh, H, head);
-    const __amdgpu_buffer_rsrc_t rq = make_rsrc(Q + head * D, (uint32_t)L * D * 4);
-    const __amdgpu_buffer_rsrc_t rg = make_rsrc(dO + head * D, (uint32_t)L * D * 4);
-    const __amdgpu_buffer_rsrc_t rc = make_rsrc(FIXED ? Q : gate + head, (uint32_t)L * 4);
-    const __amdgpu_buffer_rsrc_t rl = make_rsrc(LSE + head, (uint32_t)L * 4);
-    const __amdgpu_buffer_rsrc_t rd = make_rsrc(delta + head, (uint32_t)L * 4);
-    const float c_k0 = gr.raw(k0);
-    const float ck = k_valid ? gr.diff(kj, k0) : 0.0f;
-    float dc = 0.0f;
-    auto issue_q = [&](int j) {
-      f32_dma_tile<D>(rq, sm.tile[wave][0], dma_off, 32 * j);
-      const uint32_t off = (uint32_t)(32 * j + lane) * 4;
-      if constexpr (!FIXED) dma4(rc, &sm.row[wave][0][0], off);
-      dma4(rl, &sm.row[wave][1][0], off);
-      dma4(rd, &sm.row[wave][2][0], off);
-    };
-    auto issue_g = [&](int j) { f32_dma_tile<D>(rg, sm.tile[wave][1], dma_off, 32 * j); };
-    if (kb + wave < n_tiles) {
-      issue_q(kb + wave);
-      issue_g(kb + wave);
-    }
-    for (int j = kb + wave; j < n_tiles; j += NW) {
-      const bool more = j + NW < n_tiles;
-      wait_vmem6<NL>();  // Q and the row statistics of tile j; its dO may still load
-      f32x16 s = {};
-      f32_row_product<D>(qt, kf, s);
-      wait_vmem6<0>();  // dO of tile j
-      f32x16 dp = {};
-      f32_row_product<D>(gt, vf, dp);
-      float p[16], ds[16];
+      const GateRow<FIXED> gr(gate, bh, H, head);
+      const __amdgpu_buffer_rsrc_t rq = make_rsrc(Q + head * D, (uint32_t)L * D * 4);
+      const __amdgpu_buffer_rsrc_t rg = make_rsrc(dO + head * D, (uint32_t)L * D * 4);
+      const __amdgpu_buffer_rsrc_t rc = make_rsrc(FIXED ? Q : gate + head, (uint32_t)L * 4);
+      const __amdgpu_buffer_rsrc_t rl = make_rsrc(LSE + head, (uint32_t)L * 4);
+      const __amdgpu_buffer_rsrc_t rd = make_rsrc(delta + head, (uint32_t)L * 4);
+      const float c_k0 = gr.raw(k0);
+      const float ck = k_valid ? gr.diff(kj, k0) : 0.0f;
+      float dc = 0.0f;
+      auto issue_q = [&](int j) {
+        f32_dma_tile<D>(rq, sm.tile[wave][0], dma_off, 32 * j);
+        const uint32_t off = (uint32_t)(32 * j + lane) * 4;
+        if constexpr (!FIXED) dma4(rc, &sm.row[wave][0][0], off);
+        dma4(rl, &sm.row[wave][1][0], off);
+        dma4(rd, &sm.row[wave][2][0], off);
+      };
+      auto issue_g = [&](int j) { f32_dma_tile<D>(rg, sm.tile[wave][1], dma_off, 32 * j); };
+      if (kb + wave < n_tiles) {
+        issue_q(kb + wave);
+        issue_g(kb + wave);
+      }
+      for (int j = kb + wave; j < n_tiles; j += NW) {
+        const bool more = j + NW < n_tiles;
+        wait_vmem6<NL>();  // Q and the row statistics of tile j; its dO may still load
+        f32x16 s = {};
+        f32_row_product<D>(qt, kf, s);
+        wait_vmem6<0>();  // dO of tile j
+        f32x16 dp = {};
+        f32_row_product<D>(gt, vf, dp);
+        float p[16], ds[16];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 c4 = FIXED ? f32x4{} : *(const lds_f32x4_t*)(row_at + 32 * g);
-        const f32x4 l4 = *(const lds_f32x4_t*)(row_at + 256 + 32 * g);
-        const f32x4 d4 = *(const lds_f32x4_t*)(row_at + 512 + 32 * g);
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 c4 = FIXED ? f32x4{} : *(const lds_f32x4_t*)(row_at + 32 * g);
+          const f32x4 l4 = *(const lds_f32x4_t*)(row_at + 256 + 32 * g);
+          const f32x4 d4 = *(const lds_f32x4_t*)(row_at + 512 + 32 * g);
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) {
-          const int r = 4 * g + jj, qq = 32 * j + 8 * g + 4 * h + jj;
-          const float cq = gr.diff_raw(qq, c4[jj], k0, c_k0);
-          p[r] = exp2_fast(s[r] * scale_log2 + ((cq - ck) - l4[jj]) * kLog2e);
-          p[r] = qq >= kj && qq < L ? p[r] : 0.0f;
-          ds[r] = p[r] * (dp[r] - d4[jj]);
-          dc -= ds[r];
+          for (int jj = 0; jj < 4; ++jj) {
+            const int r = 4 * g + jj, qq = 32 * j + 8 * g + 4 * h + jj;
+            const float cq = gr.diff_raw(qq, c4[jj], k0, c_k0);
+            p[r] = exp2_fast(s[r] * scale_log2 + ((cq - ck) - l4[jj]) * kLog2e);
+            p[r] = qq >= kj && qq < L ? p[r] : 0.0f;
+            ds[r] = p[r] * (dp[r] - d4[jj]);
+            dc -= ds[r];
+          }
         }
+        f32_tr_product<D>(qt, ds, ak);
+        sched_fence();  // every read of the Q tile and of the row statistics is done
+        if (more) issue_q(j + NW);
+        f32_tr_product<D>(gt, p, av);
+        sched_fence();  // every read of the dO tile is done
+        if (more) issue_g(j + NW);
       }
-      f32_tr_product<D>(qt, ds, ak);
-      sched_fence();  // every read of the Q tile and of the row statistics is done
-      if (more) issue_q(j + NW);
-      f32_tr_product<D>(gt, p, av);
-      sched_fence();  // every read of the dO tile is done
-      if (more) issue_g(j + NW);
-    }
-    const float dct = wave_sum_pair(dc);
-    if (h == 0) sm.dc[wave][col] = dct;
-    if constexpr (PK) {  // dc^k belongs to a query head
-      __syncthreads();
-      if (tid < 32 && k0 + tid < L) {
-        float dt = 0.0f;
+      const float dct = wave_sum_pair(dc);
+      if (h == 0) sm.dc[wave][col] = dct;
+      if constexpr (PK) {  // dc^k belongs to a query head
+        __syncthreads();
+        if (tid < 32 && k0 + tid < L) {
+          float dt = 0.0f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) dt += sm.dc[w][tid];
-        dck[head + k0 + tid] = dt;
+          for (int w = 0; w < NW; ++w) dt += sm.dc[w][tid];
+          dck[head + k0 + tid] = dt;
+        }
+        __syncthreads();  // the next head writes the sums again
       }
-      __syncthreads();  // the next head writes the sums again
     }
-    }  // query heads
 
     f32_put_partial<D>(sm.tile[wave][0], ak, col, h);
     f32_put_partial<D>(sm.tile[wave][1], av, col, h);

@@ -50,7 +50,7 @@ struct PackedPlace {
 };
 __device__ __forceinline__ bool packed_place(const PackedItem* __restrict__ plan, int bid, int H,
                                              int Hkv, int N, PackedPlace& p) {
-  const PackedItem it = plan[bid / H];
+  const PackedItem it = packed_item(plan, bid / H, N);
   p.len = it.len;
   p.block = it.block;
   p.head = packed_head(bid % H, Hkv, H / Hkv);
@@ -720,7 +720,7 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   static_assert(NDMA >= 1 && NDMA * kPkPairs * 1024 == TILE * 2, "the P waves cover a tile");
   __shared__ __attribute__((aligned(16))) PkKvSmem<D, BM> sm;
 
-  const PackedItem item = plan[blockIdx.x / (Hkv * splits)];
+  const PackedItem item = packed_item(plan, blockIdx.x / (Hkv * splits), N);
   if (item.len <= 0) return;
   // the query heads of this workgroup: group hg of G heads of the key head's
   const int L = item.len, hk = (int)(blockIdx.x % Hkv), hg = (int)(blockIdx.x / Hkv % splits);

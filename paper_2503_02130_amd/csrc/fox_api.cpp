@@ -91,6 +91,16 @@ bool cache_dtype(int dtype) { return dtype == FOX_DTYPE_F32 || dtype == FOX_DTYP
 
 constexpr int kMaxNewTokens = 64;
 
+// New tokens of a call.  Its largest launch has a workgroup of 256 for each of the B H n rows.
+bool cache_new_ok(const fox_cache_t* c, int n) {
+  return n >= 1 && n <= kMaxNewTokens && (long long)c->B * c->H * n <= (1LL << 22);
+}
+// Rows of a copy to or from the cache, for each head c and for each key head d / 8 threads.
+bool cache_rows_ok(const fox_cache_t* c, long long rows) {
+  return rows > 0 && rows * c->H <= (1LL << 31) - 1 &&
+         rows * (c->H + (long long)c->H_kv * (c->d / 8)) < (1LL << 32) - 1024;
+}
+
 int cache_max_len(const fox_cache_t* c, int max_len) {
   const int cap = c->max_pages * c->page;
   return max_len <= 0 || max_len > cap ? cap : max_len;
@@ -875,7 +885,7 @@ fox_status_t fox_cache_append(const fox_cache_t* cache, fox_dtype_t dtype, const
   fox_status_t st = check_cache(cache);
   if (st) return st;
   if (!all_set({k, v, gate_logit, seq_len})) return FOX_ERR_NULL;
-  if (n < 1 || n > kMaxNewTokens) return FOX_ERR_SHAPE;
+  if (!cache_new_ok(cache, n)) return FOX_ERR_SHAPE;
   if (!cache_dtype(dtype)) return FOX_ERR_UNSUPPORTED;
   if (!all_aligned16({k, v, gate_logit, seq_len, parent, n_new})) return FOX_ERR_ALIGN;
   return launch_status(fox::launch_cache_append(cache_spec(cache), dtype == FOX_DTYPE_BF16, k, v,
@@ -888,7 +898,7 @@ fox_status_t fox_cache_append_packed(const fox_cache_t* cache, fox_dtype_t dtype
   fox_status_t st = check_cache(cache);
   if (st) return st;
   if (!all_set({k, v, c, cu_seqlens})) return FOX_ERR_NULL;
-  if (N < 1 || (long long)N * cache->H > (1LL << 31) - 1) return FOX_ERR_SHAPE;
+  if (!cache_rows_ok(cache, N)) return FOX_ERR_SHAPE;
   if (!cache_dtype(dtype)) return FOX_ERR_UNSUPPORTED;
   if (!all_aligned16({k, v, c, cu_seqlens, seq_len})) return FOX_ERR_ALIGN;
   return launch_status(fox::launch_cache_append_packed(cache_spec(cache), dtype == FOX_DTYPE_BF16,
@@ -911,7 +921,7 @@ fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const i
   fox_status_t st = check_cache(cache);
   if (st) return st;
   if (!all_set({seq_len, k, v})) return FOX_ERR_NULL;
-  if (T < 1 || (long long)T * cache->B * cache->H > (1LL << 31) - 1) return FOX_ERR_SHAPE;
+  if (!cache_rows_ok(cache, (long long)T * cache->B)) return FOX_ERR_SHAPE;
   if (!cache_dtype(dtype)) return FOX_ERR_UNSUPPORTED;
   if (!all_aligned16({start, seq_len, k, v, c})) return FOX_ERR_ALIGN;
   return launch_status(fox::launch_cache_read(cache_spec(cache), dtype == FOX_DTYPE_BF16, start,
@@ -919,7 +929,7 @@ fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const i
 }
 
 size_t fox_attn_cache_workspace_bytes(const fox_cache_t* cache, int n, int max_len) {
-  if (check_cache(cache) || n < 1 || n > kMaxNewTokens) return 0;
+  if (check_cache(cache) || !cache_new_ok(cache, n)) return 0;
   return fox::attn_cache_workspace_bytes(cache_spec(cache), n, cache_max_len(cache, max_len));
 }
 
@@ -929,7 +939,7 @@ fox_status_t fox_attn_cache(const fox_cache_t* cache, const void* q, const int* 
   fox_status_t st = check_cache(cache);
   if (st) return st;
   if (!all_set({q, seq_len, o, lse})) return FOX_ERR_NULL;
-  if (n < 1 || n > kMaxNewTokens) return FOX_ERR_SHAPE;
+  if (!cache_new_ok(cache, n)) return FOX_ERR_SHAPE;
   if (!all_aligned16({q, seq_len, parent, n_new, o, lse, workspace})) return FOX_ERR_ALIGN;
   const fox::CacheSpec s = cache_spec(cache);
   const int len = cache_max_len(cache, max_len);

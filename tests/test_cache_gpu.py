@@ -279,7 +279,8 @@ def test_pages_that_do_not_exist(fmt):
 
 
 def test_one_row_alone_and_in_a_batch():
-    """What other sequences hold does not change a sequence's bits."""
+    """A sequence short enough for one piece has the same bits beside any others; the same call
+    gives the same bits."""
     cache = Cache(3, 4, 2, 128, 64, 8, "e4m3", 71)
     cache.fill([400, 100, 257])
     q = torch.randn((3, 4, 1, 128), device=DEV, generator=cache.g).to(torch.bfloat16)

@@ -11,6 +11,10 @@ pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 
 
+def _ints(x):
+    return torch.tensor(x, device=DEV, dtype=torch.int32)
+
+
 def _inputs(H, Hkv, d, lens, dtype, gate_dtype, seed, behind=0, mean=(0.0, 5.0)):
     g = torch.Generator(device=DEV)
     g.manual_seed(seed)
@@ -133,6 +137,23 @@ def test_lengths_out_of_range_stay_inside(cu):
     for start, length, block, seq in plan.view(-1, 4).tolist():
         assert 0 <= start and 0 <= length and start + length <= N
         assert length == 0 or (128 * block < length and 0 <= seq < len(cu) - 1)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_plan_of_another_batch_stays_inside(dtype):
+    """A list of as many places made for more rows: its blocks lie outside and are skipped."""
+    H, d, N = 2, 64, 130
+    plan = fox.fox_packed_plan(_ints([0, 200, 255]), 255)
+    q, k, v, o = (torch.full((H, N, d), 7.0, device=DEV, dtype=dtype) for _ in range(4))
+    x = torch.full((H, N), 7.0, device=DEV)
+    cu = _ints([0, 100, 130])
+    lse = x.clone()
+    fox.fox_attn_fwd_packed(q, k, v, x, cu, plan, o=o, lse=lse)
+    assert (o == 7).all() and (lse == 7).all()
+    grads = [torch.full_like(q, 7.0) for _ in range(3)]
+    fox.fox_attn_bwd_packed(q, k, v, x, o, lse, q, x, cu, plan, dq=grads[0], dk=grads[1],
+                            dv=grads[2])
+    assert all((g == 7).all() for g in grads)
 
 
 @pytest.mark.parametrize("d", [64, 128])
