@@ -82,7 +82,8 @@ __device__ __forceinline__ int v_swizzle(int key) {
 
 // The ancestors of new token `lane`, whose parent is `up`, and itself, as bits (pointers doubled).
 __device__ __forceinline__ uint64_t ancestors(int up, int nn, int lane) {
-  uint64_t bits = 1ull << lane;
+  const uint32_t bit = 1u << (lane & 31);
+  uint64_t bits = lane < 32 ? (uint64_t)bit : (uint64_t)bit << 32;
   if (lane >= nn || up >= lane) up = -1;
   while (__any(up >= 0)) {
     const int from = up >= 0 ? up : lane;
@@ -220,12 +221,15 @@ __device__ __forceinline__ void ca_scores(float* x, const f32x4& s, const f32x4&
 __device__ __forceinline__ float ca_base(float m) { return m == kCaFloor ? 0.0f : m; }
 
 // The mask of a lane's four keys of a half in a tile that holds keys from `valid` on, which do
-// not exist, or new tokens (from kk = 0 on), of which only ancestors are seen.
+// not exist, or new tokens (from kk = 0 on), of which only ancestors are seen.  The bit is
+// taken from one half of the 64: v_lshrrev_b64 with its shift in the last of 256 registers,
+// where the compiler had put it, shifted by something else now and then.
 __device__ __forceinline__ void ca_mask(float* u, int valid, int kk0, uint64_t anc) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int kk = kk0 + j;
-    const int seen = (int)(j < valid) & ((int)(kk < 0) | (int)((anc >> (kk & 63)) & 1));
+    const uint32_t half = kk & 32 ? (uint32_t)(anc >> 32) : (uint32_t)anc;
+    const int seen = (int)(j < valid) & ((int)(kk < 0) | (int)((half >> (kk & 31)) & 1));
     u[j] = seen ? u[j] : -INFINITY;
   }
 }

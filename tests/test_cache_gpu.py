@@ -209,6 +209,8 @@ ATTN = [
     ("e4m3", 4, 4, 128, 128, 64, [60, 128, 1000, 7], True),
     ("bf16", 10, 2, 64, 16, 33, [5, 0, 90, 400], True),     # 165 rows: row blocks
     ("e4m3", 32, 1, 64, 32, 1, [100, 5, 31, 600], False),   # 32 heads to a key head
+    ("e4m3", 16, 2, 128, 128, 64, [3001, 1041, 60, 1001], True),  # 512 rows, two row tiles
+    ("bf16", 16, 2, 128, 16, 64, [0, 1041, 60, 1001], True),
 ]
 
 
@@ -276,6 +278,25 @@ def test_pages_that_do_not_exist(fmt):
     fox.fox_cache_append(cache.dev, kn, vn, logit, ints([16, 60, 1 << 30]), None, ints([n, n, n]))
     fox.fox_cache_keep(cache.dev, ints([14, 60, 64]), ints([[3, 2, 1, 0]] * 3), ints([2, 4, 4]))
     assert all(torch.equal(a, b) for a, b in zip(before, cache.snapshot()))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+def test_same_bits_on_a_full_device(fmt, d):
+    """Many rows on many workgroups: every wave of every call gives the same bits.  The lengths
+    put the new tokens at different places of a tile."""
+    n, lens = 64, [3001, 7441, 5033, 4000]
+    cache = Cache(4, 16, 2, d, 128, 60, fmt, 61)
+    cache.fill([x + n for x in lens])
+    g = torch.Generator()
+    g.manual_seed(2)
+    parents = [_random_tree(n, g) for _ in lens]
+    q = torch.randn((4, 16, n, d), device=DEV, generator=cache.g).to(torch.bfloat16)
+    first = fox.fox_attn_cache(q, cache.dev, ints(lens), ints(parents))
+    _attn_check(cache, lens, [n] * 4, parents, q, *first, fox.default_scale(d))
+    for _ in range(20):
+        again = fox.fox_attn_cache(q, cache.dev, ints(lens), ints(parents))
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
 def test_one_row_alone_and_in_a_batch():
