@@ -521,7 +521,7 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  * other, without padding.  Query head h reads key head h / (H / H_kv) and has its own forget
  * gate; H is a multiple of H_kv.
  *
- *   q, o, d_o, dq  [H,N,d] dtype     k, v, dk, dv  [H_kv,N,d] dtype
+ *   q, o, o_lo, d_o, dq  [H,N,d] dtype     k, v, dk, dv  [H_kv,N,d] dtype
  *   gate logits    [H,N] fp32 or bf16 (gate_dtype)     c, lse [H,N] fp32
  *   cu_seqlens     [B+1] int32, on the device: sequence b is rows cu_seqlens[b] ..
  *                  cu_seqlens[b+1] - 1; the first is 0, the last at most N, none is smaller
@@ -539,9 +539,12 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  *   (summed in 64 bits, rounded once).
  * fox_attn_fwd_packed: O and LSE of each sequence as fox_attn_fwd's.  max_len: the longest
  *   sequence, if known, else 0 (N): it decides how the work is split, not what is computed.
+ *   o_lo (bf16, may be NULL): what rounding took from o, for the backward.
  * fox_attn_bwd_packed: the gradients of sum(O o dO): dq, dk, dv (dk, dv summed over the query
  *   heads of a key head) and d_logit in gate_dtype, the gradient of the gate logits; d_log_f
- *   [H,N] fp32, that of log f, may be NULL.  With zero_behind not 0 the gradients' rows
+ *   [H,N] fp32, that of log f, may be NULL.  With o_lo (bf16, may be NULL) the row sums of
+ *   dO o O that dq needs come from o + o_lo: its relative error is then about 2.4e-3 in place
+ *   of 2.7e-3 (rounding dq alone: 1.7e-3).  With zero_behind not 0 the gradients' rows
  *   behind the last sequence are set to zero.  workspace: at least
  *   fox_attn_bwd_packed_workspace_bytes() for the same max_len.
  * fox_packed_zero_behind: writes zeros to the rows behind the last sequence of n (at most 8)
@@ -560,13 +563,13 @@ fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_log
                            const int* cu_seqlens, float* c, int B, int H, int N,
                            hipStream_t stream);
 fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
-                        const float* c, const void* plan, void* o, float* lse, int B, int H,
+                        const float* c, const void* plan, void* o, void* o_lo, float* lse, int B, int H,
                         int H_kv, int N, int d, int max_len, float scale, hipStream_t stream);
 size_t fox_attn_bwd_packed_workspace_bytes(fox_dtype_t dtype, int H, int H_kv, int N, int d,
                                            int max_len);
 fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
-                        const float* c, const void* o, const float* lse, const void* d_o,
-                        fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
+                        const float* c, const void* o, const void* o_lo, const float* lse,
+                        const void* d_o, fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
                         const void* plan, void* dq, void* dk, void* dv, void* d_logit,
                         float* d_log_f, int zero_behind, void* workspace,
                         size_t workspace_bytes, int B, int H, int H_kv, int N, int d,

@@ -177,8 +177,8 @@ def load() -> ctypes.CDLL:
             ("fox_attn_cache", [P, P, P, P, P, P, P, P, Z, I, I, F, P]),
             ("fox_packed_plan", [P, I, I, P, Z, P, I, P]),
             ("fox_gate_prefix_packed", [I, P, P, P, I, I, I, P]),
-            ("fox_attn_fwd_packed", [I, P, P, P, P, P, P, P, I, I, I, I, I, I, F, P]),
-            ("fox_attn_bwd_packed", [I, P, P, P, P, P, P, P, I, P, P, P, P, P, P, P, P, I, P, Z,
+            ("fox_attn_fwd_packed", [I, P, P, P, P, P, P, P, P, I, I, I, I, I, I, F, P]),
+            ("fox_attn_bwd_packed", [I, P, P, P, P, P, P, P, P, I, P, P, P, P, P, P, P, P, I, P, Z,
                                      I, I, I, I, I, I, F, P]),
             ("fox_packed_zero_behind", [P, I, P, I, I, P])):
         getattr(lib, name).restype = I

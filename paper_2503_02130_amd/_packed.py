@@ -81,11 +81,12 @@ def fox_gate_prefix_packed(gate_logit: torch.Tensor, cu_seqlens: torch.Tensor,
 def fox_attn_fwd_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c: torch.Tensor,
                         cu_seqlens: torch.Tensor, plan: Optional[torch.Tensor] = None,
                         max_len: int = 0, scale: Optional[float] = None,
-                        o: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
-                        ) -> Tuple[torch.Tensor, torch.Tensor]:
+                        o: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                        o_lo: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """O [H,N,d] (q's dtype) and LSE [H,N] fp32 of packed sequences: q [H,N,d], k, v
     [H_kv,N,d] bf16 or fp32, c from fox_gate_prefix_packed, plan from fox_packed_plan.
-    max_len: the longest sequence, if known.  Rows behind the last sequence are not written."""
+    max_len: the longest sequence, if known.  o_lo (bf16), if given, is filled with what rounding
+    took from O, for the backward.  Rows behind the last sequence are not written."""
     H, Hkv, N, d = _check_qkv(q, k, v)
     dev = q.device
     _need(c, "c", (H, N), torch.float32, dev)
@@ -102,9 +103,11 @@ def fox_attn_fwd_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c: to
         lse = torch.empty((H, N), device=dev, dtype=torch.float32)
     else:
         _need(lse, "lse", (H, N), torch.float32, dev)
+    if o_lo is not None:
+        _need(o_lo, "o_lo", (H, N, d), torch.bfloat16, dev)
     s = default_scale(d) if scale is None else float(scale)
     st = _call(load().fox_attn_fwd_packed, dev, _DT[q.dtype], _ptr(q), _ptr(k), _ptr(v), _ptr(c),
-               _ptr(plan), _ptr(o), _ptr(lse), B, H, Hkv, N, d, max_len, s)
+               _ptr(plan), _ptr(o), _ptr(o_lo), _ptr(lse), B, H, Hkv, N, d, max_len, s)
     _raise(st, "fox_attn_fwd_packed")
     return o, lse
 
@@ -117,14 +120,16 @@ def fox_attn_bwd_packed_workspace_bytes(dtype: torch.dtype, H: int, H_kv: int, N
 def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
                         cu_seqlens: torch.Tensor, plan: Optional[torch.Tensor] = None,
                         max_len: int = 0, scale: Optional[float] = None, dq=None, dk=None,
-                        dv=None, d_logit=None, d_log_f=None, workspace=None):
+                        dv=None, d_logit=None, d_log_f=None, workspace=None, o_lo=None):
     """dq [H,N,d], dk, dv [H_kv,N,d] and d_logit [H,N] (the gate logits' dtype, fp32 or bf16)
-    of sum(o * d_o); d_log_f [H,N] fp32 is filled if given.  Rows behind the last sequence are
+    of sum(o * d_o); d_log_f [H,N] fp32 is filled if given; o_lo as the forward left it.  Rows behind the last sequence are
     not written."""
     H, Hkv, N, d = _check_qkv(q, k, v)
     dt, dev = q.dtype, q.device
     for name, t in (("o", o), ("d_o", d_o)):
         _need(t, name, (H, N, d), dt, dev)
+    if o_lo is not None:
+        _need(o_lo, "o_lo", (H, N, d), torch.bfloat16, dev)
     for name, t in (("c", c), ("lse", lse)):
         _need(t, name, (H, N), torch.float32, dev)
     gdt = gate_logit.dtype
@@ -154,8 +159,8 @@ def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
         nbytes = _workspace_bytes(workspace, dev)
     s = default_scale(d) if scale is None else float(scale)
     st = _call(lib.fox_attn_bwd_packed, dev, _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(o),
-               _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), _ptr(cu_seqlens), _ptr(plan),
-               _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_logit), _ptr(d_log_f), 0, _ptr(workspace),
+               _ptr(o_lo), _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), _ptr(cu_seqlens),
+               _ptr(plan), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_logit), _ptr(d_log_f), 0, _ptr(workspace),
                nbytes, B, H, Hkv, N, d, max_len, s)
     _raise(st, "fox_attn_bwd_packed")
     return dq, dk, dv, d_logit
@@ -178,7 +183,7 @@ def fox_packed_zero_behind(tensors: Sequence[torch.Tensor], cu_seqlens: torch.Te
 # ---------------------------------------------------------------------------
 # The two halves of an autograd step, each with one pass of checks.
 def _step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
-    """(plan, c, o, lse), o zero behind the last sequence."""
+    """(plan, c, o, o_lo, lse), o zero behind the last sequence; o_lo None for fp32."""
     H, Hkv, N, d = _check_qkv(q, k, v)
     dt, dev = _DT[q.dtype], q.device
     gdt = gate_logit.dtype
@@ -189,6 +194,7 @@ def _step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
     lib, cu = load(), _ptr(cu_seqlens)
     c, lse = (torch.empty((H, N), device=dev, dtype=torch.float32) for _ in range(2))
     o = torch.empty_like(q)
+    o_lo = torch.empty_like(q) if q.dtype == torch.bfloat16 else None
     row = _RowsStruct(_ptr(o), H, d * o.element_size())
     if plan is None:
         places = _plan_places(B, N)
@@ -202,13 +208,14 @@ def _step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
     _raise(_call(lib.fox_gate_prefix_packed, dev, _DT[gdt], _ptr(gate_logit), cu, _ptr(c), B, H, N),
            "fox_gate_prefix_packed")
     _raise(_call(lib.fox_attn_fwd_packed, dev, dt, _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(plan),
-                 _ptr(o), _ptr(lse), B, H, Hkv, N, d, max_len, scale), "fox_attn_fwd_packed")
-    return plan, c, o, lse
+                 _ptr(o), _ptr(o_lo), _ptr(lse), B, H, Hkv, N, d, max_len, scale),
+           "fox_attn_fwd_packed")
+    return plan, c, o, o_lo, lse
 
 
 def _step_backward(saved, d_o, max_len, scale):
     """dq, dk, dv, d_logit, zero behind the last sequence, from what the forward checked."""
-    q, k, v, gate_logit, c, o, lse, cu_seqlens, plan = saved
+    q, k, v, gate_logit, c, o, o_lo, lse, cu_seqlens, plan = saved
     (H, N, d), Hkv, B = q.shape, k.shape[0], cu_seqlens.shape[0] - 1
     dt, gdt, dev = q.dtype, gate_logit.dtype, q.device
     _need(d_o, "d_o", (H, N, d), dt, dev)
@@ -218,7 +225,7 @@ def _step_backward(saved, d_o, max_len, scale):
     nbytes = lib.fox_attn_bwd_packed_workspace_bytes(_DT[dt], H, Hkv, N, d, max_len)
     ws = _workspace(nbytes, dev)
     _raise(_call(lib.fox_attn_bwd_packed, dev, _DT[dt], _ptr(q), _ptr(k), _ptr(v), _ptr(c),
-                 _ptr(o), _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), cu, _ptr(plan),
-                 *map(_ptr, grads), None, 1, _ptr(ws), nbytes, B, H, Hkv, N, d, max_len, scale),
+                 _ptr(o), _ptr(o_lo), _ptr(lse), _ptr(d_o), _DT[gdt], _ptr(gate_logit), cu,
+                 _ptr(plan), *map(_ptr, grads), None, 1, _ptr(ws), nbytes, B, H, Hkv, N, d, max_len, scale),
            "fox_attn_bwd_packed")
     return grads

@@ -62,9 +62,9 @@ class PackedForgettingAttention(torch.autograd.Function):
     def forward(ctx, q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
         gate_logit = gate_logit.contiguous()
-        plan, c, o, lse = _packed._step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len,
-                                                scale)
-        ctx.save_for_backward(q, k, v, gate_logit, c, o, lse, cu_seqlens, plan)
+        plan, c, o, o_lo, lse = _packed._step_forward(q, k, v, gate_logit, cu_seqlens, plan,
+                                                      max_len, scale)
+        ctx.save_for_backward(q, k, v, gate_logit, c, o, o_lo, lse, cu_seqlens, plan)
         ctx.max_len, ctx.scale = max_len, scale
         return o
 

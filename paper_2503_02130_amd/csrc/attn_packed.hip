@@ -23,7 +23,9 @@
 //     backward forms dS from P rounded to fp16 (2^-12 of it; carried as 2^15 P,
 //     which fp16 holds to full precision down to 2^-29) and dc^k adds the unrounded fp32 dS.
 //   * c_i shifts a whole softmax row, so dc^q = rowsum(dS) is 0; what it comes out as is the
-//     error of Delta, formed from O as rounded to bf16.  The dQ kernel runs first and adds its
+//     error of Delta, formed from O as rounded to bf16 (or, with o_lo, from O in which only P
+//     was: dQ, which takes the Delta that it starts from, is then 2.4e-3 off and not 2.7e-3,
+//     where dQ's own rounding is 1.7e-3, for 1% of a training step).  The dQ kernel runs first and adds its
 //     row sums (of dS in fp32) to Delta: the dK/dV kernel then sees the Delta of its own P,
 //     rows of dS that sum to 0 to fp32 rounding, and d(log f) is the reverse sum of dc^k
 //     alone.  bf16 rounding is left in the operands dS and, for dV, P.
@@ -78,7 +80,7 @@ template <int D, int KS>
 __global__ __launch_bounds__(kPkThreads * KS) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2)))
 void packed_fwd_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
                        const bf16* __restrict__ V, const float* __restrict__ C,
-                       bf16* __restrict__ O, float* __restrict__ LSE,
+                       bf16* __restrict__ O, bf16* __restrict__ Olo, float* __restrict__ LSE,
                        const PackedItem* __restrict__ plan, int H, int Hkv, int N,
                        float scale_log2) {
   constexpr int TILE = kPkBN * D;
@@ -376,15 +378,21 @@ void packed_fwd_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   const float l_tot = wave_sum_pair(l_run);
   if (q_valid) {
     const float inv = 1.0f / l_tot;
-    bf16* orow = O + (at.row + qi) * D;
+    const size_t row = (at.row + qi) * D;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        bf16x4 w;
+        const size_t e = row + db * 32 + 8 * g + 4 * h;
+        bf16x4 w, lo;
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) w[jj] = to_bf16(oacc[db][4 * g + jj] * inv);
-        *reinterpret_cast<bf16x4*>(orow + db * 32 + 8 * g + 4 * h) = w;
+        for (int jj = 0; jj < 4; ++jj) {
+          const float x = oacc[db][4 * g + jj] * inv;
+          w[jj] = to_bf16(x);
+          lo[jj] = to_bf16(x - to_f32(w[jj]));
+        }
+        *reinterpret_cast<bf16x4*>(O + e) = w;
+        if (Olo) *reinterpret_cast<bf16x4*>(Olo + e) = lo;
       }
     if (h == 0) LSE[at.row + qi] = (c[qi] - c_q0) + kLn2 * (m_used + log2f(l_tot));
   }
@@ -432,8 +440,8 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
 void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
                       const bf16* __restrict__ V, const float* __restrict__ C,
                       const float* __restrict__ LSE, const bf16* __restrict__ dO,
-                      const bf16* __restrict__ O, float* __restrict__ delta,
-                      bf16* __restrict__ dQ, const PackedItem* __restrict__ plan, int H, int Hkv,
+                      const bf16* __restrict__ O, const bf16* __restrict__ Olo,
+                      float* __restrict__ delta, bf16* __restrict__ dQ, const PackedItem* __restrict__ plan, int H, int Hkv,
                       int N, float scale, float scale_log2) {
   constexpr int TILE = kPkBN * D;
   constexpr int NDMA = TILE * 2 / 1024 / kPkWaves;
@@ -477,13 +485,17 @@ void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   const float lse_q = q_valid ? LSE[at.row + qi] : 0.0f;
   // Delta_i = dO_i . O_i: a lane holds half of its row's dims, in the pieces of its operands
   float dlt = 0.0f;
-  if (q_valid) {
+  auto add_rows = [&](const bf16* x) {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      const bf16x8 ov = *reinterpret_cast<const bf16x8*>(O + (at.row + qi) * D + 16 * s + 8 * h);
+      const bf16x8 ov = *reinterpret_cast<const bf16x8*>(x + (at.row + qi) * D + 16 * s + 8 * h);
 #pragma unroll
       for (int e = 0; e < 8; ++e) dlt = __builtin_fmaf(to_f32(ov[e]), to_f32(dof[s][e]), dlt);
     }
+  };
+  if (q_valid) {
+    add_rows(O);
+    if (Olo) add_rows(Olo);
   }
   dlt = wave_sum_pair(dlt);
 
@@ -1098,12 +1110,13 @@ static bool packed_dq_split(long long wgs, int max_len) {
 }
 
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
-                             float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
+                             void* o_lo, float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s) {
   const dim3 grid((unsigned)packed_items(B, N) * (unsigned)H);
   auto run = [&](auto kernel, int groups) {
     hipLaunchKernelGGL(kernel, grid, dim3(kPkThreads * groups), 0, s, (const bf16*)q,
-                       (const bf16*)k, (const bf16*)v, c, (bf16*)o, lse, (const PackedItem*)plan,
+                       (const bf16*)k, (const bf16*)v, c, (bf16*)o, (bf16*)o_lo, lse,
+                       (const PackedItem*)plan,
                        H, Hkv, N, scale * kLog2e);
   };
   const int groups = packed_fwd_groups(d, row_blocks(H, N), max_len);
@@ -1119,8 +1132,8 @@ hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const 
 }
 
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
-                             const void* o, const float* lse, const void* d_o, void* dq, void* dk,
-                             void* dv, float* delta, float* dck, float* part,
+                             const void* o, const void* o_lo, const float* lse, const void* d_o,
+                             void* dq, void* dk, void* dv, float* delta, float* dck, float* part,
                              const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s) {
   const unsigned items = (unsigned)packed_items(B, N);
@@ -1134,7 +1147,7 @@ hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const 
   const bool split = packed_dq_split(row_blocks(H, N), max_len);
   auto qs = [&](auto kernel, int groups) {
     hipLaunchKernelGGL(kernel, dim3(items * H), dim3(kPkThreads * groups), 0, s, (const bf16*)q,
-                       (const bf16*)k, (const bf16*)v, c, lse, (const bf16*)d_o, (const bf16*)o, delta,
+                       (const bf16*)k, (const bf16*)v, c, lse, (const bf16*)d_o, (const bf16*)o, (const bf16*)o_lo, delta,
                        (bf16*)dq, (const PackedItem*)plan, H, Hkv, N, scale, scale * kLog2e);
   };
   if (d == 128) {

@@ -979,7 +979,7 @@ fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_log
 }
 
 fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
-                        const float* c, const void* plan, void* o, float* lse, int B, int H,
+                        const float* c, const void* plan, void* o, void* o_lo, float* lse, int B, int H,
                         int H_kv, int N, int d, int max_len, float scale, hipStream_t stream) {
   if (!all_set({q, k, v, c, plan, o, lse})) return FOX_ERR_NULL;
   fox_status_t st = check_packed(B, H, H_kv, N);
@@ -987,10 +987,11 @@ fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k
   if (d <= 0 || (long long)N * d * 4 >= (1LL << 31)) return FOX_ERR_SHAPE;
   st = check_dtype_d(dtype, d);
   if (st) return st;
-  if (!all_aligned16({q, k, v, c, plan, o, lse})) return FOX_ERR_ALIGN;
+  if (o_lo && dtype != FOX_DTYPE_BF16) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({q, k, v, c, plan, o, o_lo, lse})) return FOX_ERR_ALIGN;
   const int len = max_len <= 0 || max_len > N ? N : max_len;
   if (dtype == FOX_DTYPE_BF16)
-    return launch_status(fox::launch_packed_fwd(q, k, v, c, o, lse, plan, B, H, H_kv, N, d, len,
+    return launch_status(fox::launch_packed_fwd(q, k, v, c, o, o_lo, lse, plan, B, H, H_kv, N, d, len,
                                                 scale, stream));
   return launch_status(fox::launch_packed_fwd_f32((const float*)q, (const float*)k,
                                                   (const float*)v, c, (float*)o, lse, plan, B, H,
@@ -1007,8 +1008,8 @@ size_t fox_attn_bwd_packed_workspace_bytes(fox_dtype_t dtype, int H, int H_kv, i
 }
 
 fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
-                        const float* c, const void* o, const float* lse, const void* d_o,
-                        fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
+                        const float* c, const void* o, const void* o_lo, const float* lse,
+                        const void* d_o, fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
                         const void* plan, void* dq, void* dk, void* dv, void* d_logit,
                         float* d_log_f, int zero_behind, void* workspace,
                         size_t workspace_bytes, int B, int H, int H_kv, int N, int d,
@@ -1020,8 +1021,8 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
   if (d <= 0 || (long long)N * d * 4 >= (1LL << 31)) return FOX_ERR_SHAPE;
   st = check_dtype_d(dtype, d);
   if (st) return st;
-  if (!cache_dtype(gate_dtype)) return FOX_ERR_UNSUPPORTED;
-  if (!all_aligned16({q, k, v, c, o, lse, d_o, gate_logit, cu_seqlens, plan, dq, dk, dv, d_logit,
+  if (!cache_dtype(gate_dtype) || (o_lo && dtype != FOX_DTYPE_BF16)) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({q, k, v, c, o, o_lo, lse, d_o, gate_logit, cu_seqlens, plan, dq, dk, dv, d_logit,
                       d_log_f, workspace}))
     return FOX_ERR_ALIGN;
   if (!workspace ||
@@ -1034,7 +1035,7 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
   float *dcq = delta + row, *dck = dcq + row, *part = dck + row;
   hipError_t e;
   if (dtype == FOX_DTYPE_BF16)
-    e = fox::launch_packed_bwd(q, k, v, c, o, lse, d_o, dq, dk, dv, delta, dck, part, plan,
+    e = fox::launch_packed_bwd(q, k, v, c, o, o_lo, lse, d_o, dq, dk, dv, delta, dck, part, plan,
                                cu_seqlens, B, H, H_kv, N, d, len, scale, stream);
   else
     e = fox::launch_packed_bwd_f32((const float*)q, (const float*)k, (const float*)v, c,

@@ -231,7 +231,7 @@ hipError_t launch_packed_gate_grad(bool bf16, const float* dcq, const float* dck
                                    void* d_logit, int B, int H, int N, const ZeroRows* zeros,
                                    int n_zeros, hipStream_t s);
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
-                             float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
+                             void* o_lo, float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s);
 // Groups that the query heads of a key head are split into for dK and dV; with more than one,
 // `part` holds their partial sums, fp32 [groups][2][Hkv][N][d].
@@ -240,8 +240,8 @@ hipError_t launch_packed_head_sum(bool bf16, const float* part, const int* cu, v
                                   int B, int Hkv, int N, int d, int splits, hipStream_t s);
 // dq, dk, dv and dc_k (delta: [H, N] scratch); in bf16 dc_q is 0, in fp32 it is given too
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
-                             const void* o, const float* lse, const void* d_o, void* dq, void* dk,
-                             void* dv, float* delta, float* dck, float* part,
+                             const void* o, const void* o_lo, const float* lse, const void* d_o,
+                             void* dq, void* dk, void* dv, float* delta, float* dck, float* part,
                              const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s);
 hipError_t launch_packed_fwd_f32(const float* q, const float* k, const float* v, const float* c,

@@ -135,12 +135,14 @@ def test_packed_arguments(lib):
     assert prefix(3, p, p, p, 1, 1, 10, None) == UNSUPPORTED
     assert prefix(1, p + 2, p, p, 1, 1, 10, None) == ALIGN
 
-    def fwd(dtype=1, ptrs=(P16,) * 7, B=1, H=4, Hkv=2, N=100, d=64):
+    def fwd(dtype=1, ptrs=(P16,) * 8, B=1, H=4, Hkv=2, N=100, d=64):
         return lib.fox_attn_fwd_packed(dtype, *ptrs, B, H, Hkv, N, d, 0, 0.1, None)
 
-    for i in range(7):
-        assert fwd(ptrs=tuple(None if j == i else p for j in range(7))) == NULL
-        assert fwd(ptrs=tuple(p + 4 if j == i else p for j in range(7))) == ALIGN
+    for i in range(8):
+        if i != 6:  # o_lo
+            assert fwd(ptrs=tuple(None if j == i else p for j in range(8))) == NULL
+        assert fwd(ptrs=tuple(p + 4 if j == i else p for j in range(8))) == ALIGN
+    assert fwd(dtype=0) == UNSUPPORTED  # o_lo of an fp32 o
     assert fwd(H=3) == SHAPE and fwd(N=0) == SHAPE and fwd(B=-1) == SHAPE
     assert fwd(N=1 << 23) == SHAPE  # a head's rows pass 2^31 bytes
     assert fwd(dtype=2) == UNSUPPORTED and fwd(d=32) == UNSUPPORTED
@@ -149,17 +151,18 @@ def test_packed_arguments(lib):
     assert need(1, 4, 4, 100, 64, 0) >= 3 * 4 * 100 * 4
 
     def bwd(dtype=1, gate=0, skip=None, off=None, ws=1 << 40, ws_ptr=P16, d=64):
-        a = [p] * 7
+        a = [p] * 8
         b = [p] * 7
         if skip is not None:
-            (a if skip < 7 else b)[skip % 7] = None
+            (a if skip < 8 else b)[skip % 8] = None
         if off is not None:
-            (a if off < 7 else b)[off % 7] = p + 4
+            (a if off < 8 else b)[off % 8] = p + 4
         return lib.fox_attn_bwd_packed(dtype, *a, gate, *b, None, 0, ws_ptr, ws, 1, 4, 2, 100, d, 0,
                                        0.1, None)
 
-    for i in range(14):
-        assert bwd(skip=i) == NULL and bwd(off=i) == ALIGN
+    for i in range(15):
+        assert (i == 5 or bwd(skip=i) == NULL) and bwd(off=i) == ALIGN
+    assert bwd(dtype=0) == UNSUPPORTED  # o_lo of an fp32 o
     assert bwd(gate=5) == UNSUPPORTED and bwd(d=256) == UNSUPPORTED
     assert bwd(ws=need(1, 4, 2, 100, 64, 0) - 1) == WORKSPACE and bwd(ws_ptr=None) == WORKSPACE
     rows = (_RowsStruct * 2)((p, 2, 64), (p, 2, 63))

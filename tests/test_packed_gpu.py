@@ -91,6 +91,35 @@ def test_long_rows(lens, max_len, d):
             check(n, x, ref[n], cu[-1])
 
 
+@pytest.mark.parametrize("H,Hkv,d,lens", [(4, 2, 128, [700, 1, 130]), (3, 3, 64, [333, 0, 90])])
+def test_what_rounding_took_from_o(H, Hkv, d, lens):
+    """o_lo is o's rounding error: with it o is off by the bound less o's half step, plus o_lo's
+    own.  The backward then starts from a Delta without that part, so dq moves towards the
+    exact one."""
+    q, k, v, do, logit, cu, dcu = _inputs(H, Hkv, d, lens, BF, F32, 77, 5)
+    N, scale = q.shape[1], fox.default_scale(d)
+    c = fox.fox_gate_prefix_packed(logit, dcu)
+    o_lo = torch.full_like(q, 7.0)
+    o, lse = fox.fox_attn_fwd_packed(q, k, v, c, dcu, o_lo=o_lo)
+    alone = fox.fox_attn_fwd_packed(q, k, v, c, dcu)
+    n = cu[-1]
+    assert torch.equal(alone[0][:, :n], o[:, :n]) and torch.equal(alone[1][:, :n], lse[:, :n])
+    assert (o_lo[:, n:] == 7).all()
+    assert (o_lo[:, :n].abs() <= 2.0 ** -8 * o[:, :n].abs()).all()
+    ref = reference(q, k, v, logit, c, cu, scale, do)
+    value, bound = ref["o"]
+    # o_lo's own rounding is half a step of a value of at most 2^-8 |o|
+    tight = bound - 2.0 ** -8 * value.abs() + 2.0 ** -15 * value.abs()
+    check("o + o_lo", o.double() + o_lo.double(), (value, tight), n)
+    dq = {}
+    for lo in (None, o_lo):
+        got = fox.fox_attn_bwd_packed(q, k, v, c, o, lse, do, logit, dcu, o_lo=lo)
+        for name, x in zip(("dq", "dk", "dv", "d_logit"), got):
+            check(name, x, ref[name], n)
+        dq[lo is not None] = float((got[0][:, :n].double() - ref["dq"][0][:, :n]).norm())
+    assert dq[True] < dq[False]
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_prefix_sums(dtype):
     """Rounded once from 64 bits: at most half a step of the sum and the log sigmoids' own."""
