@@ -77,7 +77,8 @@ struct alignas(256) PkFwdSmem {
 // KS groups of four waves: group g visits key tiles t_last - g, - KS, .. with its own tile
 // buffers and barrier, and the groups' O, l and m merge in LDS.
 template <int D, int KS>
-__global__ __launch_bounds__(kPkThreads * KS) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2)))
+__global__ __launch_bounds__(kPkThreads * KS)
+__attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
 void packed_fwd_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
                        const bf16* __restrict__ V, const float* __restrict__ C,
                        bf16* __restrict__ O, bf16* __restrict__ Olo, float* __restrict__ LSE,
@@ -1087,31 +1088,29 @@ int packed_head_split(bool bf16_, int H, int Hkv, int N, int d, int max_len) {
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
-// Wave groups of a workgroup that share a row block's key tiles: more than one where the grid
-// is short and the longest row's chain of tiles decides the time, by the rules of the dense
-// kernels, whose tiles these are (attn_fwd.hip, attn_bwd.hip); the workgroups are counted as the
-// rows' blocks and the longest row as max_len.  Measured with H = 16, Hkv = 4 (us, one group /
-// split): one sequence of 3001, D = 128 62.4 / 50.6 forward; D = 64 45.1 / 38.6; one of 4000,
-// H = 12, D = 64 58.5 / 44.5.
+// Two wave groups (dQ, D = 64: three) share a row block's key tiles where the grid is short and
+// the longest row's chain of tiles decides the time: up to two workgroups per CU, counted as
+// the rows' blocks, and enough tiles of the longest row to cover the merge.  Forward in
+// microseconds, one group / two, H_kv = 4: one sequence of 3001, H = 16, D = 128 62.4 / 50.6 and
+// D = 64 41.5 / 33.9; one of 4000, H = 12, D = 64 53.8 / 42.9; four of 1024, H = 8, H_kv = 2, D = 64
+// 16.9 / 15.8; beyond two per CU one of 8192, H = 12, D = 64 126.6 / 140.4 and H = 16 151 / 173.
 static long long row_blocks(int H, int N) {
   return (long long)H * ((N + kPackedBlock - 1) / kPackedBlock);
 }
-static int packed_fwd_groups(int d, long long wgs, int max_len) {
+static bool packed_fwd_split(long long wgs, int max_len) {
   const long long tiles = (max_len + kPkBN - 1) / kPkBN;
-  if (d == 64) {
-    if (wgs <= 512 && tiles >= 24 && 12 * tiles >= wgs) return 4;
-    return wgs <= 1024 && tiles >= 12 && 16 * tiles >= wgs ? 2 : 1;
-  }
-  return wgs <= 512 && tiles >= 16 && 16 * tiles >= wgs ? 2 : 1;
+  return wgs <= 512 && tiles >= 16 && 16 * tiles >= wgs;
 }
+// The whole backward with H = H_kv = 4 (so that only dQ is split): 1000 rows, D = 128 73.6 / 69.9,
+// D = 64 60.5 / 55.1; 700 rows, D = 128 55.0 / 54.1.
 static bool packed_dq_split(long long wgs, int max_len) {
   const long long tiles = (max_len + kPkBN - 1) / kPkBN;
   return wgs <= 512 && tiles >= 8 && 24 * tiles >= wgs;
 }
 
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
-                             void* o_lo, float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
-                             int max_len, float scale, hipStream_t s) {
+                             void* o_lo, float* lse, const void* plan, int B, int H, int Hkv,
+                             int N, int d, int max_len, float scale, hipStream_t s) {
   const dim3 grid((unsigned)packed_items(B, N) * (unsigned)H);
   auto run = [&](auto kernel, int groups) {
     hipLaunchKernelGGL(kernel, grid, dim3(kPkThreads * groups), 0, s, (const bf16*)q,
@@ -1119,14 +1118,13 @@ hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const 
                        (const PackedItem*)plan,
                        H, Hkv, N, scale * kLog2e);
   };
-  const int groups = packed_fwd_groups(d, row_blocks(H, N), max_len);
+  const bool split = packed_fwd_split(row_blocks(H, N), max_len);
   if (d == 128) {
-    if (groups == 1) run(packed_fwd_kernel<128, 1>, 1);
-    else run(packed_fwd_kernel<128, 2>, 2);
+    if (split) run(packed_fwd_kernel<128, 2>, 2);
+    else run(packed_fwd_kernel<128, 1>, 1);
   } else {
-    if (groups == 1) run(packed_fwd_kernel<64, 1>, 1);
-    else if (groups == 2) run(packed_fwd_kernel<64, 2>, 2);
-    else run(packed_fwd_kernel<64, 4>, 4);
+    if (split) run(packed_fwd_kernel<64, 2>, 2);
+    else run(packed_fwd_kernel<64, 1>, 1);
   }
   return hipGetLastError();
 }
