@@ -14,7 +14,8 @@
 // All of them are bound by the rows' bytes, and at small sizes by the launch.  D / 8 lanes
 // share a row, eight elements each: 16 bytes of bf16 in, 8 bytes of codes out; the row's
 // largest magnitude meets over DPP.  Each call is one launch: the first workgroups take the
-// prefix values, the rest the rows.
+// prefix values, the rest the rows.  Rows and values are counted in 32 bits (their products
+// with the heads are below 2^31), their bytes in 64.
 #include "fox_internal.h"
 #include "kv_cache.h"
 
@@ -109,8 +110,8 @@ __global__ __launch_bounds__(kCacheThreads) void cache_append_kernel(
     // lane = new token: c = c_cached + the sum of log f over its ancestors and itself, by
     // doubling pointers, in 64 bits and rounded once
     const int lane = threadIdx.x & 63;
-    const long long job = (long long)blockIdx.x * (kCacheThreads / 64) + (threadIdx.x >> 6);
-    if (job >= (long long)cv.B * cv.H) return;
+    const unsigned job = blockIdx.x * (kCacheThreads / 64) + (threadIdx.x >> 6);
+    if (job >= (unsigned)(cv.B * cv.H)) return;
     const int b = (int)(job / cv.H), h = (int)(job % cv.H);
     const int len = max(seq_len[b], 0), nn = n_new ? min(n_new[b], n) : n;
     double sum = 0.0;
@@ -137,18 +138,19 @@ __global__ __launch_bounds__(kCacheThreads) void cache_append_kernel(
   }
   constexpr int LPR = D / 8, RPB = kCacheThreads / LPR;
   const int part = threadIdx.x % LPR;
-  const long long rows = (long long)cv.B * cv.Hkv * n;
-  const long long r = (long long)(blockIdx.x - gate_groups) * RPB + threadIdx.x / LPR;
-  if (r >= rows) return;  // whole rows leave together
-  const int t = (int)(r % n), h = (int)(r / n % cv.Hkv), b = (int)(r / n / cv.Hkv);
+  const unsigned r = (blockIdx.x - gate_groups) * RPB + threadIdx.x / LPR;
+  if (r >= (unsigned)(cv.B * cv.Hkv * n)) return;  // whole rows leave together
+  // the row first: its loads are under way while its place is looked up
+  float x[8], y[8];
+  load8(k + (size_t)r * D + 8 * part, x);
+  load8(v + (size_t)r * D + 8 * part, y);
+  const unsigned bh = r / n;
+  const int t = (int)(r % n), h = (int)(bh % cv.Hkv), b = (int)(bh / cv.Hkv);
   const int len = max(seq_len[b], 0), nn = n_new ? min(n_new[b], n) : n;
   if (t >= nn || len > cv.capacity() - 1 - t) return;
   const int p = cv.page_of(b, len + t);
   if (p < 0) return;
   const size_t row = cv.kv_row(p, h, cv.slot_of(len + t));
-  float x[8], y[8];
-  load8(k + (size_t)r * D + 8 * part, x);
-  load8(v + (size_t)r * D + 8 * part, y);
   put_row<D, F8>(cv.k, cv.ke, row, part, x);
   put_row<D, F8>(cv.v, cv.ve, row, part, y);
 }
@@ -174,8 +176,8 @@ __global__ __launch_bounds__(kCacheThreads) void cache_append_packed_kernel(
     CacheView cv, const T* __restrict__ k, const T* __restrict__ v, const float* __restrict__ c,
     const int* __restrict__ cu, const int* __restrict__ seq_len, int N, unsigned gate_groups) {
   if (blockIdx.x < gate_groups) {
-    const long long i = (long long)blockIdx.x * kCacheThreads + threadIdx.x;
-    if (i >= (long long)cv.H * N) return;
+    const unsigned i = blockIdx.x * kCacheThreads + threadIdx.x;
+    if (i >= (unsigned)(cv.H * N)) return;
     const int h = (int)(i / N), r = (int)(i % N);
     const int b = packed_sequence(cu, cv.B, r);
     if (b < 0) return;
@@ -187,8 +189,11 @@ __global__ __launch_bounds__(kCacheThreads) void cache_append_packed_kernel(
   }
   constexpr int LPR = D / 8, RPB = kCacheThreads / LPR;
   const int part = threadIdx.x % LPR;
-  const long long i = (long long)(blockIdx.x - gate_groups) * RPB + threadIdx.x / LPR;
-  if (i >= (long long)cv.Hkv * N) return;
+  const unsigned i = (blockIdx.x - gate_groups) * RPB + threadIdx.x / LPR;
+  if (i >= (unsigned)(cv.Hkv * N)) return;
+  float x[8], y[8];  // the row first, as above
+  load8(k + (size_t)i * D + 8 * part, x);
+  load8(v + (size_t)i * D + 8 * part, y);
   const int h = (int)(i / N), r = (int)(i % N);
   const int b = packed_sequence(cu, cv.B, r);
   if (b < 0) return;
@@ -197,9 +202,6 @@ __global__ __launch_bounds__(kCacheThreads) void cache_append_packed_kernel(
   const int p = cv.page_of(b, len + t);
   if (p < 0) return;
   const size_t row = cv.kv_row(p, h, cv.slot_of(len + t));
-  float x[8], y[8];
-  load8(k + (size_t)i * D + 8 * part, x);
-  load8(v + (size_t)i * D + 8 * part, y);
   put_row<D, F8>(cv.k, cv.ke, row, part, x);
   put_row<D, F8>(cv.v, cv.ve, row, part, y);
 }
@@ -316,9 +318,9 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(
   };
   int slot;
   if (blockIdx.x < gate_groups) {
-    const long long i = (long long)blockIdx.x * kCacheThreads + threadIdx.x;
-    if (i >= (long long)cv.B * cv.H * T_) return;
-    const int t = (int)(i % T_), h = (int)(i / T_ % cv.H), b = (int)(i / T_ / cv.H);
+    const unsigned i = blockIdx.x * kCacheThreads + threadIdx.x, bh = i / T_;
+    if (i >= (unsigned)(cv.B * cv.H * T_)) return;
+    const int t = (int)(i % T_), h = (int)(bh % cv.H), b = (int)(bh / cv.H);
     const int p = page(b, t, slot);
     if (p >= 0) c[i] = cv.c[cv.c_at(p, h, slot)];
     else if (zero_others) c[i] = 0.0f;
@@ -326,9 +328,9 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(
   }
   constexpr int LPR = D / 8, RPB = kCacheThreads / LPR;
   const int part = threadIdx.x % LPR;
-  const long long r = (long long)(blockIdx.x - gate_groups) * RPB + threadIdx.x / LPR;
-  if (r >= (long long)cv.B * cv.Hkv * T_) return;
-  const int t = (int)(r % T_), h = (int)(r / T_ % cv.Hkv), b = (int)(r / T_ / cv.Hkv);
+  const unsigned r = (blockIdx.x - gate_groups) * RPB + threadIdx.x / LPR, bh = r / T_;
+  if (r >= (unsigned)(cv.B * cv.Hkv * T_)) return;
+  const int t = (int)(r % T_), h = (int)(bh % cv.Hkv), b = (int)(bh / cv.Hkv);
   const int p = page(b, t, slot);
   T *ko = k + (size_t)r * D + 8 * part, *vo = v + (size_t)r * D + 8 * part;
   if (p >= 0) {
