@@ -7,9 +7,10 @@
 //     u_ij = log2(e) (s 2^ek_j (q_i . k~_j) + c_i - c_j),   p_ij = 2^(u_ij - m_i),
 //     o_i = sum_j p_ij 2^ev_j v~_j / sum_j p_ij,            lse_i = ln 2 (m_i + log2 sum_j p_ij)
 //
-// with k~, v~ the codes and 2^ek, 2^ev the rows' scales (1 for a bf16 cache): K's scale
-// multiplies a score, V's a weight, so the codes go to the matrix cores unscaled (exact in
-// bf16) and no element is multiplied on its way.
+// with k~, v~ the codes and 2^ek, 2^ev the rows' scales (1 for a bf16 cache).  A lane holds codes
+// of one key, whose scale the conversion to bf16 applies (exact; keys whose values are below
+// 2^-117 may lose digits that no score sees).  V's scale multiplies a weight, and its codes
+// go to the matrix cores unscaled.
 //
 //   * The G n rows of a key head share its keys: rows are r = g n + t, 16 to a tile, RT tiles
 //     to a workgroup.  The products are 16x16x32 bf16: S^T = K Q^T (keys on the MFMA's rows,
@@ -173,8 +174,8 @@ struct CaParts {
 // Operand `st` of the first product (16 keys, dims in the order of ca_dim) from a lane's
 // 16-byte pieces of its key.
 template <bool F8>
-__device__ __forceinline__ bf16x8 k_operand(const u32x4d* w, int st) {
-  if constexpr (F8) return e4m3_operand(w[st >> 1][2 * (st & 1)], w[st >> 1][2 * (st & 1) + 1]);
+__device__ __forceinline__ bf16x8 k_operand(const u32x4d* w, int st, float scale) {
+  if constexpr (F8) return e4m3_operand(w[st >> 1][2 * (st & 1)], w[st >> 1][2 * (st & 1) + 1], scale);
   else return __builtin_bit_cast(bf16x8, w[st]);
 }
 // first of the eight dims that a lane of group grp holds in operand st
@@ -183,20 +184,14 @@ __device__ __forceinline__ int ca_dim(int st, int grp) {
   return F8 ? 64 * (st >> 1) + 16 * grp + 8 * (st & 1) : 32 * st + 8 * grp;
 }
 
-// The scales of a lane's four keys: s log2(e) 2^ek for the scores, 2^ev for the weights (bf16
-// caches: one value and none).
+// The scales 2^ev of a lane's four keys, which multiply their weights.
 template <bool F8>
 struct CaScales {
-  float k[F8 ? 4 : 1], v[F8 ? 4 : 1];
-  __device__ __forceinline__ void set(uint32_t ke, uint32_t ve, float scale_log2) {
+  float v[F8 ? 4 : 1];
+  __device__ __forceinline__ void set(uint32_t ve) {
     if constexpr (F8) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        k[j] = scale_log2 * e4m3_scale((ke >> (8 * j)) & 255u);
-        v[j] = e4m3_scale((ve >> (8 * j)) & 255u);
-      }
-    } else {
-      k[0] = scale_log2;
+      for (int j = 0; j < 4; ++j) v[j] = e4m3_scale((ve >> (8 * j)) & 255u);
     }
   }
   // The scales of keys that do not exist are whatever lies there; their weights are 0.
@@ -206,16 +201,14 @@ struct CaScales {
       for (int j = 0; j < 4; ++j) v[j] = j < valid ? v[j] : 0.0f;
     }
   }
-  __device__ __forceinline__ float ks(int j) const { return k[F8 ? j : 0]; }
 };
 
 // Scores in base 2, less `base`, of a lane's four keys of a half.
-template <bool F8>
 __device__ __forceinline__ void ca_scores(float* x, const f32x4& s, const f32x4& c, float ci,
-                                          const CaScales<F8>& sc, float base) {
+                                          float scale_log2, float base) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    x[j] = __builtin_fmaf(s[j], sc.ks(j), __builtin_fmaf(ci - c[j], kLog2e, -base));
+    x[j] = __builtin_fmaf(s[j], scale_log2, __builtin_fmaf(ci - c[j], kLog2e, -base));
 }
 // What the scores of a row are taken relative to: its running maximum, once it has seen a key.
 __device__ __forceinline__ float ca_base(float m) { return m == kCaFloor ? 0.0f : m; }
@@ -274,12 +267,13 @@ __device__ __forceinline__ void ca_softmax(float* x, const CaScales<F8>* sc, flo
   }
 }
 
-// The prefix values of a lane's four keys (c_off: of its head in a page) and the keys' scales,
-// of 16 keys that start at slot `slot` of page p.
+// Of 16 keys that start at slot `slot` of page p: the prefix values of the four whose scores a
+// lane gets (c_off: of its head in a page), V's scale exponents of these and K's of the one
+// whose codes it holds.
 template <bool F8, int RT>
 __device__ __forceinline__ void ca_load_c(const CacheView& cv, int p, int hk, int slot,
-                                          const uint32_t (&c_off)[RT], int grp, f32x4* c,
-                                          uint32_t& ke, uint32_t& ve) {
+                                          const uint32_t (&c_off)[RT], int col, int grp,
+                                          f32x4* c, uint32_t& ke, uint32_t& ve) {
   const __amdgpu_buffer_rsrc_t rc = uniform_rsrc(
       reinterpret_cast<const char*>(cv.c + cv.c_at(p, 0, 0)), (uint32_t)(cv.H << cv.page_shift) * 4);
 #pragma unroll
@@ -289,7 +283,7 @@ __device__ __forceinline__ void ca_load_c(const CacheView& cv, int p, int hk, in
     const size_t row = cv.kv_row(p, hk, slot);
     const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(reinterpret_cast<const char*>(cv.ke + row), 16);
     const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(reinterpret_cast<const char*>(cv.ve + row), 16);
-    ke = __builtin_amdgcn_raw_buffer_load_b32(rk, 4 * grp, 0, 0);
+    ke = __builtin_amdgcn_raw_buffer_load_b8(rk, col, 0, 0);
     ve = __builtin_amdgcn_raw_buffer_load_b32(rv, 4 * grp, 0, 0);
   }
 }
@@ -429,7 +423,7 @@ void attn_cache_kernel(
       for (int i = 0; i < KL; ++i)
         t.h[hf].k[i] = __builtin_bit_cast(
             u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0, 0));
-      ca_load_c<F8, RT>(cv, p, hk, slot, rows.c_off, grp, t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
+      ca_load_c<F8, RT>(cv, p, hk, slot, rows.c_off, col, grp, t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
       // V: place s of the tile holds piece (s % CPR) ^ swizzle of key s / CPR
 #pragma unroll
       for (int i = 0; i < VL / 2; ++i) {
@@ -501,7 +495,7 @@ void attn_cache_kernel(
       for (int i = 0; i < RT; ++i) s[i][hf] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < NS; ++st) {
-        const bf16x8 ka = k_operand<F8>(cur.h[hf].k, st);
+        const bf16x8 ka = k_operand<F8>(cur.h[hf].k, st, e4m3_scale(cur.h[hf].ke));
 #pragma unroll
         for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, rows.q[i][st], s[i][hf]);
       }
@@ -510,7 +504,7 @@ void attn_cache_kernel(
     bf16x8 pb[RT];
     CaScales<F8> sc[2];
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) sc[hf].set(cur.h[hf].ke, cur.h[hf].ve, scale_log2);
+    for (int hf = 0; hf < 2; ++hf) sc[hf].set(cur.h[hf].ve);
     if (!plain)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) sc[hf].clear_from(cur.valid[hf] - 4 * grp);
@@ -519,7 +513,7 @@ void attn_cache_kernel(
       float x[8];
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
-        ca_scores<F8>(x + 4 * hf, s[i][hf], cur.h[hf].c[i], rows.ci[i], sc[hf], ca_base(m[i]));
+        ca_scores(x + 4 * hf, s[i][hf], cur.h[hf].c[i], rows.ci[i], scale_log2, ca_base(m[i]));
       if (!plain)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
@@ -535,7 +529,7 @@ void attn_cache_kernel(
 #pragma unroll
     for (int db = 0; db < NB; ++db) {
       bf16x8 v;
-      if constexpr (F8) v = e4m3_operand((uint32_t)v8[db][0], (uint32_t)v8[db][1]);
+      if constexpr (F8) v = e4m3_operand((uint32_t)v8[db][0], (uint32_t)v8[db][1], 1.0f);
       else v = va[db];
 #pragma unroll
       for (int i = 0; i < RT; ++i) oacc[i][db] = mfma16(v, pb[i], oacc[i][db]);
@@ -706,7 +700,7 @@ void attn_cache_rows_kernel(
       const bool there = cv.page_exists(pg[hf]) && key < T;
       const int p = __builtin_amdgcn_readfirstlane(there ? pg[hf] : 0);
       t.valid[hf] = there ? min(16, T - key) : 0;
-      ca_load_c<F8, RT>(cv, p, hk, slot, rows.c_off, grp, t.c[hf], t.ke[hf], t.ve[hf]);
+      ca_load_c<F8, RT>(cv, p, hk, slot, rows.c_off, col, grp, t.c[hf], t.ke[hf], t.ve[hf]);
     }
   };
 
@@ -767,7 +761,7 @@ void attn_cache_rows_kernel(
       for (int i = 0; i < RT; ++i) s[i][hf] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < NS; ++st) {
-        const bf16x8 ka = k_operand<F8>(kw, st);
+        const bf16x8 ka = k_operand<F8>(kw, st, e4m3_scale(t.ke[hf]));
 #pragma unroll
         for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, rows.q[i][st], s[i][hf]);
       }
@@ -776,7 +770,7 @@ void attn_cache_rows_kernel(
                        t.valid[2] == 16 && t.valid[3] == 16;
     CaScales<F8> sc[4];
 #pragma unroll
-    for (int hf = 0; hf < 4; ++hf) sc[hf].set(t.ke[hf], t.ve[hf], scale_log2);
+    for (int hf = 0; hf < 4; ++hf) sc[hf].set(t.ve[hf]);
     if (!plain)
 #pragma unroll
       for (int hf = 0; hf < 4; ++hf) sc[hf].clear_from(t.valid[hf] - 4 * grp);
@@ -786,7 +780,7 @@ void attn_cache_rows_kernel(
       float x[16];
 #pragma unroll
       for (int hf = 0; hf < 4; ++hf)
-        ca_scores<F8>(x + 4 * hf, s[i][hf], t.c[hf][i], rows.ci[i], sc[hf], ca_base(m[i]));
+        ca_scores(x + 4 * hf, s[i][hf], t.c[hf][i], rows.ci[i], scale_log2, ca_base(m[i]));
       if (!plain)
 #pragma unroll
         for (int hf = 0; hf < 4; ++hf)
@@ -808,7 +802,7 @@ void attn_cache_rows_kernel(
         lds_wait8<0>(w);
 #pragma unroll
         for (int db = 0; db < NB; ++db) {
-          const bf16x8 v = e4m3_operand((uint32_t)w[db][0], (uint32_t)w[db][1]);
+          const bf16x8 v = e4m3_operand((uint32_t)w[db][0], (uint32_t)w[db][1], 1.0f);
 #pragma unroll
           for (int i = 0; i < RT; ++i) oacc[i][db] = mfma16(v, pb[i][P], oacc[i][db]);
         }

@@ -74,16 +74,16 @@ __device__ __forceinline__ float e4m3_inverse(uint32_t biased) {
   return __uint_as_float((254u - biased) << 23);
 }
 
-// four e4m3 codes to bf16 (exact)
-__device__ __forceinline__ void e4m3_to_bf16(uint32_t w, bf16x2& lo, bf16x2& hi) {
-  lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+// four e4m3 codes times a power of two to bf16
+__device__ __forceinline__ void e4m3_to_bf16(uint32_t w, float scale, bf16x2& lo, bf16x2& hi) {
+  lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
 }
 // eight consecutive codes as one MFMA operand
-__device__ __forceinline__ bf16x8 e4m3_operand(uint32_t a, uint32_t b) {
+__device__ __forceinline__ bf16x8 e4m3_operand(uint32_t a, uint32_t b, float scale) {
   bf16x2 p[4];
-  e4m3_to_bf16(a, p[0], p[1]);
-  e4m3_to_bf16(b, p[2], p[3]);
+  e4m3_to_bf16(a, scale, p[0], p[1]);
+  e4m3_to_bf16(b, scale, p[2], p[3]);
   bf16x8 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
