@@ -50,9 +50,6 @@ constexpr int kCaThreads = 64 * kCaWaves;
 constexpr int kCaTile = 32;                        // keys of a wave's tile
 constexpr int kCaRound = kCaWaves * kCaTile;       // keys of one turn of the waves
 constexpr float kCaSum = 256.0f;                   // a lane's tile sum above it rescales
-// Workgroups that the keys are split for, and the least units of keys of a piece.
-constexpr long long kCaWant = 2048, kCrWant = 512;
-constexpr int kCaMin = 2, kCrMin = 4;
 constexpr float kCaFloor = -1e30f;                 // the maximum before the first key
 
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
@@ -347,15 +344,14 @@ struct CaRows {
   }
 };
 
-template <int D, int RT>
+template <int D>
 struct CaMerge {
-  float o[kCaWaves][16][D + 4];  // one row tile at a time
-  float m[kCaWaves][16 * RT], l[kCaWaves][16 * RT];
+  float o[kCaWaves][16][D + 4];
+  float m[kCaWaves][16], l[kCaWaves][16];
 };
 
-template <int D, bool F8, int RT>
-__global__ __launch_bounds__(kCaThreads)
-__attribute__((amdgpu_waves_per_eu(D == 64 ? (RT == 1 ? 4 : 3) : (RT == 1 ? 3 : 2))))
+template <int D, bool F8>
+__global__ __launch_bounds__(kCaThreads) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3)))
 void attn_cache_kernel(
     CacheView cv, const bf16* __restrict__ Q, const int* __restrict__ seq_len,
     const int* __restrict__ parent, const int* __restrict__ n_new, bf16* __restrict__ O,
@@ -370,7 +366,7 @@ void attn_cache_kernel(
   constexpr int VBYTES = kCaTile * D * ESZ;
   union Smem {
     char v[kCaWaves][VBYTES];
-    CaMerge<D, RT> merge;
+    CaMerge<D> merge;
   };
   __shared__ __attribute__((aligned(1024))) Smem sm;
 
@@ -390,11 +386,11 @@ void attn_cache_kernel(
     parts.table[b] = make_int2(pc.first, pc.count);
   const int col = lane & 15, grp = lane >> 4;
 
-  CaRows<D, F8, RT> rows;
-  rows.place(cv, pc, rb * RT * 16 + col, hk, G, n, grp);
+  CaRows<D, F8, 1> rows;
+  rows.place(cv, pc, rb * 16 + col, hk, G, n, grp);
   struct Half {       // 16 keys of one page
     u32x4d k[KL];
-    f32x4 c[RT];
+    f32x4 c;
     uint32_t ke, ve;
   };
   struct Tile {
@@ -423,7 +419,7 @@ void attn_cache_kernel(
       for (int i = 0; i < KL; ++i)
         t.h[hf].k[i] = __builtin_bit_cast(
             u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0, 0));
-      ca_load_c<F8, RT>(cv, p, hk, slot, rows.c_off, col, grp, t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
+      ca_load_c<F8, 1>(cv, p, hk, slot, rows.c_off, col, grp, &t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
       // V: place s of the tile holds piece (s % CPR) ^ swizzle of key s / CPR
 #pragma unroll
       for (int i = 0; i < VL / 2; ++i) {
@@ -462,15 +458,10 @@ void attn_cache_kernel(
   if (first < k1) issue(last, pg, cur);
   lookup(last - kCaRound, pg);
   rows.load(cv, pc, Q, parent, n, lane, grp);
-  f32x4 oacc[RT][NB];
-  float m[RT], l[RT];
+  f32x4 oacc[NB];
+  float m = rows.ok[0] ? kCaFloor : 0.0f, l = 0.0f;
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    m[i] = rows.ok[i] ? kCaFloor : 0.0f;
-    l[i] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < NB; ++db) oacc[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int db = 0; db < NB; ++db) oacc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int key0 = last; key0 >= first; key0 -= kCaRound) {
     wait_all_memory();
     sched_fence();
@@ -488,39 +479,32 @@ void attn_cache_kernel(
     }
 
     // S^T of the two halves
-    f32x4 s[RT][2];
+    f32x4 s[2];
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
+      s[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < RT; ++i) s[i][hf] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int st = 0; st < NS; ++st) {
-        const bf16x8 ka = k_operand<F8>(cur.h[hf].k, st, e4m3_scale(cur.h[hf].ke));
-#pragma unroll
-        for (int i = 0; i < RT; ++i) s[i][hf] = mfma16(ka, rows.q[i][st], s[i][hf]);
-      }
+      for (int st = 0; st < NS; ++st)
+        s[hf] = mfma16(k_operand<F8>(cur.h[hf].k, st, e4m3_scale(cur.h[hf].ke)), rows.q[0][st], s[hf]);
     }
     const bool plain = cur.valid[0] == 16 && cur.valid[1] == 16 && key0 + kCaTile <= len;
-    bf16x8 pb[RT];
+    bf16x8 pb;
     CaScales<F8> sc[2];
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) sc[hf].set(cur.h[hf].ve);
     if (!plain)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) sc[hf].clear_from(cur.valid[hf] - 4 * grp);
+    float x[8];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      float x[8];
+    for (int hf = 0; hf < 2; ++hf)
+      ca_scores(x + 4 * hf, s[hf], cur.h[hf].c, rows.ci[0], scale_log2, ca_base(m));
+    if (!plain)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
-        ca_scores(x + 4 * hf, s[i][hf], cur.h[hf].c[i], rows.ci[i], scale_log2, ca_base(m[i]));
-      if (!plain)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
-          ca_mask(x + 4 * hf, rows.ok[i] ? cur.valid[hf] - 4 * grp : 0,
-                  key0 + 16 * hf + 4 * grp - len, rows.anc[i]);
-      ca_softmax<F8, NB, 2>(x, sc, m[i], l[i], oacc[i], &pb[i]);
-    }
+        ca_mask(x + 4 * hf, rows.ok[0] ? cur.valid[hf] - 4 * grp : 0,
+                key0 + 16 * hf + 4 * grp - len, rows.anc[0]);
+    ca_softmax<F8, NB, 2>(x, sc, m, l, oacc, &pb);
     sched_fence();
     wait_lds();  // V is in registers
     if (key0 > first) issue(key0 - kCaRound, pg, cur);
@@ -531,64 +515,55 @@ void attn_cache_kernel(
       bf16x8 v;
       if constexpr (F8) v = e4m3_operand((uint32_t)v8[db][0], (uint32_t)v8[db][1], 1.0f);
       else v = va[db];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) oacc[i][db] = mfma16(v, pb[i], oacc[i][db]);
+      oacc[db] = mfma16(v, pb, oacc[db]);
     }
   }
 
   // merge the waves
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const float lt = group_sum(l[i]);
-    if (grp == 0) {
-      sm.merge.m[wave][16 * i + col] = m[i];
-      sm.merge.l[wave][16 * i + col] = lt;
-    }
+  const float lt = group_sum(l);
+  __syncthreads();  // the V tiles are done with
+  if (grp == 0) {
+    sm.merge.m[wave][col] = m;
+    sm.merge.l[wave][col] = lt;
   }
   __syncthreads();
+  float M = kCaFloor;
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    float M = kCaFloor;
+  for (int w = 0; w < kCaWaves; ++w) M = fmaxf(M, sm.merge.m[w][col]);
+  const float f = exp2_fast(m - M);
 #pragma unroll
-    for (int w = 0; w < kCaWaves; ++w) M = fmaxf(M, sm.merge.m[w][16 * i + col]);
-    const float f = exp2_fast(m[i] - M);
+  for (int db = 0; db < NB; ++db)
+    *reinterpret_cast<f32x4*>(&sm.merge.o[wave][col][16 * db + 4 * grp]) = oacc[db] * f;
+  __syncthreads();
+  for (int item = threadIdx.x; item < 16 * (D / 4); item += kCaThreads) {
+    const int rr = item / (D / 4), e = item % (D / 4) * 4;
+    const int r = rb * 16 + rr, g = r / n, t = r - g * n;
+    if (g >= G || t >= nn) continue;
+    float Mr = kCaFloor, lr = 0.0f;
 #pragma unroll
-    for (int db = 0; db < NB; ++db)
-      *reinterpret_cast<f32x4*>(&sm.merge.o[wave][col][16 * db + 4 * grp]) = oacc[i][db] * f;
-    __syncthreads();
-    for (int item = threadIdx.x; item < 16 * (D / 4); item += kCaThreads) {
-      const int rr = item / (D / 4), e = item % (D / 4) * 4;
-      const int r = (rb * RT + i) * 16 + rr;
-      const int g = r / n, t = r - g * n;
-      if (g >= G || t >= nn) continue;
-      float Mr = kCaFloor, lr = 0.0f;
+    for (int w = 0; w < kCaWaves; ++w) Mr = fmaxf(Mr, sm.merge.m[w][rr]);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kCaWaves; ++w) Mr = fmaxf(Mr, sm.merge.m[w][16 * i + rr]);
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < kCaWaves; ++w) {
+      lr += sm.merge.l[w][rr] * exp2_fast(sm.merge.m[w][rr] - Mr);
+      o += *reinterpret_cast<const f32x4*>(&sm.merge.o[w][rr][e]);
+    }
+    const size_t R = ((size_t)b * cv.H + hk * G + g) * n + t;
+    if (pc.count == 1) {
+      const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;  // a row without a key: zeros, -inf
+      bf16x4 w4;
 #pragma unroll
-      for (int w = 0; w < kCaWaves; ++w) {
-        lr += sm.merge.l[w][16 * i + rr] * exp2_fast(sm.merge.m[w][16 * i + rr] - Mr);
-        o += *reinterpret_cast<const f32x4*>(&sm.merge.o[w][rr][e]);
-      }
-      const size_t R = ((size_t)b * cv.H + hk * G + g) * n + t;
-      if (pc.count == 1) {
-        const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;  // a row without a key: zeros, -inf
-        bf16x4 w4;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w4[j] = to_bf16(o[j] * inv);
-        *reinterpret_cast<bf16x4*>(O + R * D + e) = w4;
-        if (e == 0) LSE[R] = lr > 0.0f ? kLn2 * (Mr + log2f(lr)) : -INFINITY;
-      } else {
-        const size_t at = ((size_t)(pc.first + pc.split) * cv.H + hk * G + g) * n + t;
-        *reinterpret_cast<f32x4*>(parts.o + at * D + e) = o;
-        if (e == 0) {
-          parts.ml[2 * at] = Mr;
-          parts.ml[2 * at + 1] = lr;
-        }
+      for (int j = 0; j < 4; ++j) w4[j] = to_bf16(o[j] * inv);
+      *reinterpret_cast<bf16x4*>(O + R * D + e) = w4;
+      if (e == 0) LSE[R] = lr > 0.0f ? kLn2 * (Mr + log2f(lr)) : -INFINITY;
+    } else {
+      const size_t at = ((size_t)(pc.first + pc.split) * cv.H + hk * G + g) * n + t;
+      *reinterpret_cast<f32x4*>(parts.o + at * D + e) = o;
+      if (e == 0) {
+        parts.ml[2 * at] = Mr;
+        parts.ml[2 * at + 1] = lr;
       }
     }
-    if (i + 1 < RT) __syncthreads();
   }
 }
 
@@ -919,6 +894,28 @@ __global__ __launch_bounds__(D / 4 * SG) void attn_cache_join_kernel(
 // ---------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------
+// Which kernel.  The one whose waves split the keys reads K without a detour and has more of
+// them in flight; the one that shares tiles reads and converts them once for 64 or 128 rows.
+// us at 32 sequences of 8000 tokens, H_kv = 4, split / shared: bf16, d = 128 4 rows 103 / 99,
+// 24 rows 132 / 105; d = 64 16 rows 49 / 53, 24 rows 60 / 55; e4m3, d = 128 32 rows 74 / 82, 40
+// rows 95 / 82; d = 64 32 rows 40 / 66, 64 rows 63 / 66; a single sequence of 2000, 4 rows 10.6 / 12.1.
+// Two row tiles to a wave halve the tiles' reads and conversions but need twice the rows: 128
+// rows, H_kv = 2, d = 128 two / one e4m3 67 / 78, bf16 72 / 78, but one sequence of 2000 with
+// H_kv = 4 19.3 / 15.7 and 18.0 / 14.1, one of 16000 27.5 / 26.9 and 24.5 / 22.8.
+constexpr long long kCrTwo = 1 << 17;  // keys of all workgroups from which two row tiles pay
+// How many workgroups the keys are split for.  Sharing: as many as are resident, two or
+// three to a CU (512 / 768 / 1024 workgroups: e4m3, one row tile 90 / 82 / 87 us; bf16, d = 128 119 /
+// 131 / 124; two row tiles, 64 drafts of four sequences, 54 / 64 / 68).  Splitting waves: far more,
+// so that sequences of different lengths even out (512 / 1024 / 2048 / 4096: 64 sequences of
+// 8 to 32 thousand tokens 286 / 264 / 260 / 259 us).
+constexpr long long kCaWant = 2048, kCrWant2 = 512, kCrWant3 = 768;
+// The least keys of a piece, 256, 512 or 1024, by the keys of all workgroups: small calls want
+// short pieces, larger ones fewer to start and to join.  256 / 512 / 1024, H_kv = 4, e4m3, d = 128:
+// one sequence of 2000 9.8 / 11.8 / 15.5 us; one of 30000 17.7 / 15.9 / 19.0; 32 of 2000 22.4 / 19.4 /
+// 20.2; 128 of 1000 36.9 / 33.0 / 26.3 (not split).  Sharing, 1024 leaves CUs idle where the
+// lengths differ: 64 drafts of four sequences of 3 to 16 thousand tokens 51 / 51 / 66.
+constexpr long long kCaSome = 80000, kCaMany = 500000;
+
 struct CaPlan {
   bool shared;  // the kernel for many rows
   int rt, n_rowblk, n_pieces;
@@ -927,14 +924,17 @@ struct CaPlan {
 static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
   CaPlan p;
   const int rows = s.H / s.Hkv * n;
-  p.shared = rows > 32;
-  p.rt = p.shared ? (rows <= 64 ? 1 : 2) : rows <= 16 ? 1 : 2;
-  const int per = 16 * p.rt * (p.shared ? kCaWaves : 1);
-  p.n_rowblk = (rows + per - 1) / per;
+  const long long seqs = (long long)s.B * s.Hkv;
+  p.shared = rows > (s.f8 ? (s.d == 64 ? 64 : 32) : 16);
+  auto blocks = [&](int rt) { return (rows + 64 * rt - 1) / (64 * rt); };
+  p.rt = p.shared && rows > 64 && seqs * blocks(2) * max_len >= kCrTwo ? 2 : 1;
+  p.n_rowblk = p.shared ? blocks(p.rt) : (rows + 15) / 16;
+  const long long all = seqs * p.n_rowblk * max_len;  // keys of all workgroups, at most
+  const int least = all < kCaSome ? 256 : all < kCaMany || p.shared ? 512 : 1024;
+  const long long want = !p.shared ? kCaWant : p.rt == 2 || (s.d == 128 && !s.f8) ? kCrWant2 : kCrWant3;
   p.split.unit = p.shared ? kCrTile : kCaRound;
-  p.split.min_units = p.shared ? kCrMin : kCaMin;
-  const long long want = (p.shared ? kCrWant : kCaWant) / ((long long)s.Hkv * p.n_rowblk);
-  p.split.target = (int)std::max<long long>(1, want);
+  p.split.min_units = (least + p.split.unit - 1) / p.split.unit;
+  p.split.target = (int)std::max<long long>(1, want / ((long long)s.Hkv * p.n_rowblk));
   // no more than sequences of max_len make, and none where each is one least piece; longer
   // ones are then cut into larger pieces
   const long long units = ((long long)max_len + p.split.unit - 1) / p.split.unit;
@@ -973,13 +973,9 @@ hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_l
   auto by_rows = [&](auto dc, auto f8) {
     constexpr int D = decltype(dc)::value;
     constexpr bool F8 = decltype(f8)::value;
-    if (p.shared) {
-      if (p.rt == 1) run(attn_cache_rows_kernel<D, F8, 1>);
-      else run(attn_cache_rows_kernel<D, F8, 2>);
-    } else {
-      if (p.rt == 1) run(attn_cache_kernel<D, F8, 1>);
-      else run(attn_cache_kernel<D, F8, 2>);
-    }
+    if (!p.shared) run(attn_cache_kernel<D, F8>);
+    else if (p.rt == 1) run(attn_cache_rows_kernel<D, F8, 1>);
+    else run(attn_cache_rows_kernel<D, F8, 2>);
   };
   auto by_format = [&](auto dc) {
     if (s.f8) by_rows(dc, std::true_type());
