@@ -350,7 +350,14 @@ struct CaMerge {
   float m[kCaWaves][16], l[kCaWaves][16];
 };
 
-template <int D, bool F8>
+// NT: K and V bypass the caches (read once, and more than they hold).
+template <bool NT>
+__device__ __forceinline__ void ca_dma16(__amdgpu_buffer_rsrc_t r, void* lds, uint32_t off) {
+  if constexpr (NT) dma16_nt(r, lds, off);
+  else dma16(r, lds, off);
+}
+
+template <int D, bool F8, bool NT>
 __global__ __launch_bounds__(kCaThreads) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3)))
 void attn_cache_kernel(
     CacheView cv, const bf16* __restrict__ Q, const int* __restrict__ seq_len,
@@ -418,14 +425,15 @@ void attn_cache_kernel(
 #pragma unroll
       for (int i = 0; i < KL; ++i)
         t.h[hf].k[i] = __builtin_bit_cast(
-            u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0, 0));
+            u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0,
+                                                           NT ? kNonTemporal : 0));
       ca_load_c<F8, 1>(cv, p, hk, slot, rows.c_off, col, grp, &t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
       // V: place s of the tile holds piece (s % CPR) ^ swizzle of key s / CPR
 #pragma unroll
       for (int i = 0; i < VL / 2; ++i) {
         const int s = i * 64 + lane, kr = s / CPR;
         const int piece = (s % CPR) ^ v_swizzle<D, F8>(16 * hf + kr);
-        dma16(rv, vbuf + (hf * (VL / 2) + i) * 1024, (uint32_t)(kr * D * ESZ + 16 * piece));
+        ca_dma16<NT>(rv, vbuf + (hf * (VL / 2) + i) * 1024, (uint32_t)(kr * D * ESZ + 16 * piece));
       }
     }
   };
@@ -604,7 +612,7 @@ struct CrSmem {
   char v[2][kCrTile * D * (F8 ? 1 : 2)];
 };
 
-template <int D, bool F8, int RT>
+template <int D, bool F8, int RT, bool NT>
 __global__ __launch_bounds__(kCaThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void attn_cache_rows_kernel(
     CacheView cv, const bf16* __restrict__ Q, const int* __restrict__ seq_len,
@@ -651,9 +659,9 @@ void attn_cache_rows_kernel(
 #pragma unroll
     for (int i = 0; i < HL; ++i) {
       const int sl = i * 64 + ln, kr = sl / CPR, pc = sl % CPR;
-      dma16(rk, sm.k[B] + wave * 16 * ROW + i * 1024,
+      ca_dma16<NT>(rk, sm.k[B] + wave * 16 * ROW + i * 1024,
             (uint32_t)(kr * ROW + 16 * (pc ^ k_swizzle<D, F8>(kr))));
-      dma16(rv, sm.v[B] + wave * 16 * ROW + i * 1024,
+      ca_dma16<NT>(rv, sm.v[B] + wave * 16 * ROW + i * 1024,
             (uint32_t)(kr * ROW + 16 * (pc ^ v_swizzle<D, F8>(16 * (wave & 1) + kr))));
     }
   };
@@ -916,9 +924,16 @@ constexpr long long kCaWant = 2048, kCrWant2 = 512, kCrWant3 = 768;
 // lengths differ: 64 drafts of four sequences of 3 to 16 thousand tokens 51 / 51 / 66.
 constexpr long long kCaSome = 80000, kCaMany = 500000;
 
+// Bytes of K and V from which they bypass the caches when one row block reads them: 1.5 times
+// the 256 MB that the last level holds.  us with / without: e4m3, d = 128, 64 sequences of 20000
+// (1.3 GB) 237 / 257, 32 of 8000 (262 MB, in the cache from the call before) 60 / 53; bf16 64 of
+// 20000 430 / 477, 32 of 8000 95 / 103.
+constexpr long long kCaBypass = 384LL << 20;
+
 struct CaPlan {
   bool shared;  // the kernel for many rows
   int rt, n_rowblk, n_pieces;
+  bool once;  // keys bypass the caches
   CaSplit split;
 };
 static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
@@ -930,6 +945,7 @@ static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
   p.rt = p.shared && rows > 64 && seqs * blocks(2) * max_len >= kCrTwo ? 2 : 1;
   p.n_rowblk = p.shared ? blocks(p.rt) : (rows + 15) / 16;
   const long long all = seqs * p.n_rowblk * max_len;  // keys of all workgroups, at most
+  p.once = p.n_rowblk == 1 && all * 2 * s.d * (s.f8 ? 1 : 2) >= kCaBypass;
   const int least = all < kCaSome ? 256 : all < kCaMany || p.shared ? 512 : 1024;
   const long long want = !p.shared ? kCaWant : p.rt == 2 || (s.d == 128 && !s.f8) ? kCrWant2 : kCrWant3;
   p.split.unit = p.shared ? kCrTile : kCaRound;
@@ -973,9 +989,11 @@ hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_l
   auto by_rows = [&](auto dc, auto f8) {
     constexpr int D = decltype(dc)::value;
     constexpr bool F8 = decltype(f8)::value;
-    if (!p.shared) run(attn_cache_kernel<D, F8>);
-    else if (p.rt == 1) run(attn_cache_rows_kernel<D, F8, 1>);
-    else run(attn_cache_rows_kernel<D, F8, 2>);
+    if (p.rt == 2) run(attn_cache_rows_kernel<D, F8, 2, false>);
+    else if (p.shared && p.once) run(attn_cache_rows_kernel<D, F8, 1, true>);
+    else if (p.shared) run(attn_cache_rows_kernel<D, F8, 1, false>);
+    else if (p.once) run(attn_cache_kernel<D, F8, true>);
+    else run(attn_cache_kernel<D, F8, false>);
   };
   auto by_format = [&](auto dc) {
     if (s.f8) by_rows(dc, std::true_type());

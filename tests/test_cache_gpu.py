@@ -249,6 +249,23 @@ def test_attention_splits(fmt, max_len):
         _attn_check(cache, [3000], [3], None, q, o, lse, fox.default_scale(64))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fmt,H,n", [("e4m3", 8, 1), ("bf16", 8, 1), ("e4m3", 20, 4), ("bf16", 20, 4)])
+def test_tables_of_large_caches(fmt, H, n, d):
+    """Tables with places for far more than the caches of the device hold (the loads then bypass
+    them), nearly all without a page; 4 and 40 rows."""
+    lens = [700, 0, 1029, 250]
+    cache = Cache(4, H, 2, d, 256, 5, fmt, 55)
+    cache.fill([x + n for x in lens])
+    table = torch.full((4, 1 << 11), -1, device=DEV, dtype=torch.int32)
+    table[:, :5] = cache.table
+    wide = fox.PagedCache(cache.dev.k, cache.dev.v, cache.dev.c, table, cache.dev.k_exp,
+                          cache.dev.v_exp)
+    q = torch.randn((4, H, n, d), device=DEV, generator=cache.g).to(torch.bfloat16)
+    o, lse = fox.fox_attn_cache(q, wide, ints(lens))
+    _attn_check(cache, lens, [n] * 4, None, q, o, lse, fox.default_scale(d))
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
 def test_pages_that_do_not_exist(fmt):
     """A context page, the page of the new tokens, and places past the table."""
