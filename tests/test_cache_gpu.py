@@ -266,6 +266,34 @@ def test_tables_of_large_caches(fmt, H, n, d):
     _attn_check(cache, lens, [n] * 4, None, q, o, lse, fox.default_scale(d))
 
 
+@pytest.mark.parametrize("fmt,extra", [("e4m3", 34000), ("bf16", 17000)])
+def test_pages_behind_32_bits(fmt, extra):
+    """Pages whose places in k and v lie beyond 4 GiB: written, kept, read and attended to."""
+    B, H, Hkv, d, page, n, lens = 2, 4, 4, 128, 256, 5, [300, 7]
+    cache = Cache(B, H, Hkv, d, page, 2, fmt, 57, extra_pages=extra)
+    last = cache.dev.n_pages - 1
+    assert (last - 3) * Hkv * page * d * cache.dev.k.element_size() > 1 << 32
+    cache.table.copy_(last - torch.arange(4, device=DEV, dtype=torch.int32).view(2, 2))
+    cache.fill([x + n for x in lens])
+    q = torch.randn((B, H, n, d), device=DEV, generator=cache.g).to(torch.bfloat16)
+    o, lse = fox.fox_attn_cache(q, cache.dev, ints(lens))
+    _attn_check(cache, lens, [n] * B, None, q, o, lse, fox.default_scale(d))
+    k, v, c = fox.fox_cache_read(cache.dev, ints(lens), 300, dtype=torch.float32)
+    for b, L in enumerate(lens):
+        for got, want in ((k, cache.k), (v, cache.v), (c, cache.c)):
+            assert torch.equal(got[b][:, :L].double(), want[b][:, :L])
+    # the tokens written again, as a prompt and as new ones, and moved, are the same
+    fox.fox_cache_append_packed(cache.dev, k[:, :, :7].transpose(0, 1).reshape(Hkv, 14, d), v[
+        :, :, :7].transpose(0, 1).reshape(Hkv, 14, d), c[:, :, :7].transpose(0, 1).reshape(H, 14),
+        ints([0, 7, 14]))
+    fox.fox_cache_append(cache.dev, k[:, :, 7:9].contiguous(), v[:, :, 7:9].contiguous(),
+                         torch.zeros((B, H, 2), device=DEV), ints([7, 7]))
+    fox.fox_cache_keep(cache.dev, ints([6, 6]), ints([[2], [2]]), ints([1, 1]))
+    k2, v2, _ = fox.fox_cache_read(cache.dev, ints([9, 9]), 9, dtype=torch.float32)
+    want = torch.tensor([0, 1, 2, 3, 4, 5, 8, 7, 8], device=DEV)
+    assert torch.equal(k2[0], k[0][:, want]) and torch.equal(v2[0], v[0][:, want])
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
 def test_pages_that_do_not_exist(fmt):
     """A context page, the page of the new tokens, and places past the table."""
