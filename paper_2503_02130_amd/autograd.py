@@ -87,7 +87,12 @@ def forgetting_attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     H_kv); gate_logit: [H, N] fp32 or bf16; cu_seqlens: [B + 1] int32, sequence b being rows
     cu_seqlens[b] .. cu_seqlens[b + 1] - 1.  max_len: the longest sequence, if known (it sets
     how the work is split).  plan: fox_packed_plan(cu_seqlens, N), to share it between layers.
-    The output and the gradients are zero in rows behind the last sequence.
+    The output and the gradients are zero in rows behind the last sequence.  bf16: a tensor of
+    o's size is kept besides o (what rounding took from it) for dq.
+
+    Forward and backward may be captured into a graph, from leaves of which no eager autograd
+    graph lives (torch would wait for that graph's stream inside the capture): capture from
+    detached ones.
     """
     s = fox.default_scale(q.shape[-1]) if scale is None else float(scale)
     return PackedForgettingAttention.apply(q, k, v, gate_logit, cu_seqlens, plan, max_len, s)

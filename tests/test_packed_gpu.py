@@ -325,3 +325,37 @@ def test_step_in_a_graph():
         for n in outs:
             rows = new[-1] if n in ("o", "lse") else N
             assert torch.equal(outs[n][:, :rows], want[n][:, :rows]), (i, n)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_autograd_step_in_a_graph(dtype):
+    """forgetting_attention_packed and its backward captured and replayed with new inputs, against
+    the same step run eagerly between the replays."""
+    H, Hkv, d, lens = 4, 2, 64, [150, 70]
+    q, k, v, do, logit, cu, dcu = _inputs(H, Hkv, d, lens, dtype, F32, 23)
+    static = [q, k, v, logit]
+
+    def step():
+        leaves = [x.detach().requires_grad_() for x in static]
+        o = fox.forgetting_attention_packed(*leaves, dcu, max_len=150)
+        return (o.detach(), *torch.autograd.grad(o, leaves, do))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for i in range(4):
+        for x in (*static, do):
+            x.copy_(torch.randn(x.shape, device=DEV))
+        dcu.copy_(torch.tensor([0, 150 - 40 * i, 220 - i], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step()
+        torch.cuda.synchronize()
+        for n, (a, b) in enumerate(zip(outs, want)):
+            assert torch.equal(a, b), (i, n)
+            assert not a[:, 220 - i:].any()
