@@ -29,6 +29,12 @@
 //     row sums (of dS in fp32) to Delta: the dK/dV kernel then sees the Delta of its own P,
 //     rows of dS that sum to 0 to fp32 rounding, and d(log f) is the reverse sum of dc^k
 //     alone.  bf16 rounding is left in the operands dS and, for dV, P.
+//
+// Bound by instruction issue, as the dense kernels (matrix and vector instructions overlap in
+// part).  Prompts of 1001 to 8192 tokens, H = 16, H_kv = 4, D = 128: forward 440 us, 1.05 PFLOP/s of
+// a large library product's 1.36.  Three of 1500 to 8191: forward 394, dQ 568, dK/dV 835 us (965,
+// 1000 and 910 TFLOP/s).  Twelve of 64 to 2048, H = 12, D = 64: 52, 73 and 98 us (540, 570, 570): short
+// rows end in masked tiles and D = 64 has half the matrix work to the same exponentials.
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>

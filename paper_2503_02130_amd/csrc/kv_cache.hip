@@ -11,7 +11,10 @@
 //   read           positions start .. of each sequence as bf16 or fp32 (code times scale:
 //                  exact in both).
 //
-// All of them are bound by the rows' bytes, and at small sizes by the launch.  D / 8 lanes
+// All of them are bound by the rows' bytes, and at small sizes by the launch: 36 thousand prompt
+// tokens of H = 16, H_kv = 4, d = 128, bf16 to e4m3, are written in 27 us (119 MB, 4.4 TB/s) and read
+// back in 21 us (120 MB, 5.8 TB/s; a plain copy reaches 4.8); one token of each of 64 sequences
+// takes 3.6 us.  D / 8 lanes
 // share a row, eight elements each: 16 bytes of bf16 in, 8 bytes of codes out; the row's
 // largest magnitude meets over DPP.  Each call is one launch: the first workgroups take the
 // prefix values, the rest the rows.  Rows and values are counted in 32 bits (their products
