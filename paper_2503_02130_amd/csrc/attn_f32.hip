@@ -520,8 +520,9 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
     for (int db = 0; db < D / 32; ++db) ak[db] = av[db] = f32x16{};
     const int n_tiles = (L + 31) / 32;
 
-    // the query heads of this key head (dense: one)
-    for (int g = 0; g < G; ++g, head += PK ? pk.N : 0) {
+    float dc = 0.0f;
+    // the queries of one head, whose rows begin at `head`
+    auto query_head = [&](size_t head) {
       const GateRow<FIXED> gr(gate, bh, H, head);
       const __amdgpu_buffer_rsrc_t rq = make_rsrc(Q + head * D, (uint32_t)L * D * 4);
       const __amdgpu_buffer_rsrc_t rg = make_rsrc(dO + head * D, (uint32_t)L * D * 4);
@@ -530,7 +531,6 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
       const __amdgpu_buffer_rsrc_t rd = make_rsrc(delta + head, (uint32_t)L * 4);
       const float c_k0 = gr.raw(k0);
       const float ck = k_valid ? gr.diff(kj, k0) : 0.0f;
-      float dc = 0.0f;
       auto issue_q = [&](int j) {
         f32_dma_tile<D>(rq, sm.tile[wave][0], dma_off, 32 * j);
         const uint32_t off = (uint32_t)(32 * j + lane) * 4;
@@ -574,9 +574,16 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
         sched_fence();  // every read of the dO tile is done
         if (more) issue_g(j + NW);
       }
+    };
+    auto sum_dc = [&]() {
       const float dct = wave_sum_pair(dc);
       if (h == 0) sm.dc[wave][col] = dct;
-      if constexpr (PK) {  // dc^k belongs to a query head
+    };
+    if constexpr (PK) {  // the heads of this key head; dc^k belongs to each
+      for (int g = 0; g < G; ++g, head += pk.N) {
+        dc = 0.0f;
+        query_head(head);
+        sum_dc();
         __syncthreads();
         if (tid < 32 && k0 + tid < L) {
           float dt = 0.0f;
@@ -586,10 +593,13 @@ void bwd_dkdv_f32_kernel(const float* __restrict__ Q, const float* __restrict__ 
         }
         __syncthreads();  // the next head writes the sums again
       }
+    } else {
+      query_head(head);
     }
 
     f32_put_partial<D>(sm.tile[wave][0], ak, col, h);
     f32_put_partial<D>(sm.tile[wave][1], av, col, h);
+    if constexpr (!PK) sum_dc();
     __syncthreads();
     for (int item = tid; item < 32 * (D / 4); item += 64 * NW) {
       const int kr = item / (D / 4), chunk = item % (D / 4);
