@@ -592,7 +592,7 @@ fox_status_t fox_packed_zero_behind(const fox_packed_rows_t* tensors, int n, con
  *               of page page_table[b, t / page].  A number outside [0, n_pages) stands for
  *               no page: nothing is written there, and its tokens are not attended to.
  *               Sequences may share pages that are only read.
- *   page        16, 32, 64, 128 or 256;  d 64 or 128;  H a multiple of H_kv
+ *   page        16, 32, 64, 128 or 256;  d 64 or 128;  H a multiple of H_kv;  B at most 2^16
  *
  * The cache is the caller's memory.  Slots that hold no token may hold anything.  The calls
  * take the number of tokens that each sequence has, seq_len [B] int32 on the device, and do

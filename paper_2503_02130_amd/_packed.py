@@ -169,6 +169,8 @@ def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
 def fox_packed_zero_behind(tensors: Sequence[torch.Tensor], cu_seqlens: torch.Tensor) -> None:
     """Zeros in the rows behind the last sequence of up to 8 packed tensors [heads, N, ...]."""
     B, dev = _check_cu(cu_seqlens, None), cu_seqlens.device
+    if not 1 <= len(tensors) <= 8:
+        raise ValueError(f"1 to 8 tensors (got {len(tensors)})")
     N = tensors[0].shape[1]
     rows = (_RowsStruct * len(tensors))()
     for i, t in enumerate(tensors):

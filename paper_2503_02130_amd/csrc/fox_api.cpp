@@ -70,7 +70,8 @@ fox_status_t check_cache(const fox_cache_t* c) {
   if (c->H % c->H_kv != 0) return FOX_ERR_SHAPE;
   if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1)) != 0) return FOX_ERR_SHAPE;
   if ((long long)c->max_pages * c->page > (1LL << 30)) return FOX_ERR_SHAPE;
-  if ((long long)c->B * c->H > (1LL << 22)) return FOX_ERR_SHAPE;
+  // every workgroup of the attention looks through the lengths
+  if (c->B > (1 << 16) || (long long)c->B * c->H > (1LL << 22)) return FOX_ERR_SHAPE;
   if ((long long)c->n_pages * c->H * c->page > kMaxElems / 128) return FOX_ERR_SHAPE;
   if ((long long)c->H * c->page > (1LL << 28)) return FOX_ERR_SHAPE;  // a page of c in 32 bits
   if (c->format != FOX_CACHE_BF16 && c->format != FOX_CACHE_E4M3) return FOX_ERR_UNSUPPORTED;

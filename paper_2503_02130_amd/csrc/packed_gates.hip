@@ -98,9 +98,10 @@ __global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict_
     for (long long i = total + lane; i < n_items; i += 64) items[i] = PackedItem{0, 0, 0, -1};
 }
 
-// exp(a) on the transcendental unit: the product with log2(e) in two parts, so that large a keep
-// their digits.
+// exp(a), a <= 0, on the transcendental unit: the product with log2(e) in two parts, so that large
+// a keep their digits (from -128 on the result is 0, and the parts stay finite).
 __device__ __forceinline__ float exp_short(float a) {
+  a = fmaxf(a, -128.0f);
   const float y = a * kLog2e;
   const float lo = __builtin_fmaf(a, kLog2e, -y) + a * 1.9259629e-8f;  // log2(e) - float(log2(e))
   const float e = exp2_fast(y);

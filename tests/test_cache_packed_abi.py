@@ -38,6 +38,7 @@ BAD_CACHES = [
     (dict(n_pages=0), SHAPE), (dict(page=48), SHAPE), (dict(page=8), SHAPE), (dict(page=512), SHAPE),
     (dict(max_pages=0), SHAPE), (dict(max_pages=1 << 25), SHAPE), (dict(B=0), SHAPE),
     (dict(H=5), SHAPE), (dict(H_kv=0), SHAPE), (dict(B=1 << 12, H=1 << 12), SHAPE),
+    (dict(B=(1 << 16) + 1, H=1, H_kv=1), SHAPE),
     (dict(d=96), UNSUPPORTED), (dict(format=7), UNSUPPORTED), (dict(k=None), NULL),
     (dict(v=None), NULL), (dict(c=None), NULL), (dict(page_table=None), NULL),
     (dict(k_exp=None), NULL), (dict(v_exp=None), NULL), (dict(c=P16 + 4), ALIGN),

@@ -134,6 +134,18 @@ def test_prefix_sums(dtype):
         assert ((c[:, cu[b]:cu[b + 1]].double() - want).abs() <= tol).all()
 
 
+def test_gates_of_every_size():
+    """log sigmoid of the smallest to the largest finite logits, each a sequence of its own."""
+    x = torch.tensor([0.0, 1e-30, -1e-30, 0.5, -0.5, 17.0, -17.0, 88.0, -88.0, 104.0, -104.0, 1e4, -1e4,
+                      1e30, -1e30, 3.4e38, -3.4e38], device=DEV)
+    logit = x.view(1, -1).contiguous()
+    cu = torch.arange(x.numel() + 1, device=DEV, dtype=torch.int32)
+    c = fox.fox_gate_prefix_packed(logit, cu)[0].double()
+    want = -torch.logaddexp(torch.zeros_like(x.double()), -x.double())
+    # the function is good to a few units of its last place (and exp flushes below 2^-126)
+    assert ((c - want).abs() <= 6 * 2.0 ** -24 * want.abs() + 2.0 ** -126).all()
+
+
 def _plan_reference(lens, N):
     items, cu = [], [0]
     for x in lens:
