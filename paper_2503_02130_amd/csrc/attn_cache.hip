@@ -23,9 +23,11 @@
 //     equal pieces as workgroups are wanted, each within one sequence, from the lengths on the
 //     device (ca_piece), so a batch of ragged lengths loads the part evenly.
 //   * Splitting, the waves take 32-key tiles in turn, each with its own running maximum and
-//     sum: no barrier in the loop.  K comes straight into operand registers (a lane reads 16
-//     bytes of a key); V passes through the wave's LDS by DMA and is read back transposed.  A
-//     tile's loads are issued as soon as the registers and LDS of the one before are read.
+//     sum: no barrier in the loop.  V passes through the wave's LDS by DMA and is read back
+//     transposed; so does K where a row has 128 bytes or less (whole lines to a request: 245 ->
+//     228 us at 64 e4m3 sequences, d = 128), and longer rows, whose tiles would halve the
+//     resident workgroups, come straight into operand registers.  A tile's loads are issued
+//     as soon as the registers and LDS of the one before are read.
 //   * A tile of 32 keys is two halves of 16, each inside one page (pages hold 16 tokens or
 //     more); a half is addressed through a buffer descriptor that ends where its keys end, so
 //     nothing behind the sequence is read, and keys without a page read as zero and are masked.
@@ -37,7 +39,7 @@
 //     bf16.
 //
 // What bounds it: one token per sequence, the bytes of K and V: 64 e4m3 sequences of 8 to 32
-// thousand tokens (H = 16, H_kv = 4, d = 128, pages of 64; 1.44 GB) take 245 us, 5.9 TB/s, where a
+// thousand tokens (H = 16, H_kv = 4, d = 128, pages of 64; 1.44 GB) take 228 us, 6.3 TB/s, where a
 // plain copy of this part reaches 4.8 and a streaming read 6.6.  A single short sequence is
 // launch and latency: 2047 tokens, H = 12, d = 64 6.8 us and 2.6 to join.  Trees: 16 drafts of 16 bf16
 // sequences of 100 to 8 thousand tokens 29 us at 5.5 TB/s (and 6 to join); 64 drafts of four e4m3
@@ -86,6 +88,14 @@ __device__ __forceinline__ int v_swizzle(int key) {
   } else {
     return D == 128 ? 2 * (key & 7) : 2 * ((key >> 1) & 3);
   }
+}
+
+// Place of a 16-byte piece of K in its row: the 16 keys of a half whose pieces one operand
+// read touches lie in different banks.
+template <int D, bool F8>
+__device__ __forceinline__ int k_swizzle(int key) {
+  constexpr int BYTES = D * (F8 ? 1 : 2);
+  return BYTES == 256 ? key & 15 : BYTES == 128 ? (key >> 1) & 7 : (key >> 2) & 3;
 }
 
 // The ancestors of new token `lane`, whose parent is `up`, and itself, as bits (pointers doubled).
@@ -381,8 +391,9 @@ void attn_cache_kernel(
   constexpr int VL = kCaTile * D * ESZ / 1024;         // DMA loads of a V tile
   constexpr int NB = D / 16;                           // 16-dim blocks of O^T
   constexpr int VBYTES = kCaTile * D * ESZ;
+  constexpr bool KLDS = D * ESZ <= 128;                // K through LDS too
   union Smem {
-    char v[kCaWaves][VBYTES];
+    char v[kCaWaves][(KLDS ? 2 : 1) * VBYTES];  // V, then K
     CaMerge<D> merge;
   };
   __shared__ __attribute__((aligned(1024))) Smem sm;
@@ -406,7 +417,7 @@ void attn_cache_kernel(
   CaRows<D, F8, 1> rows;
   rows.place(cv, pc, rb * 16 + col, hk, G, n, grp);
   struct Half {       // 16 keys of one page
-    u32x4d k[KL];
+    u32x4d k[KLDS ? 1 : KL];  // without KLDS
     f32x4 c;
     uint32_t ke, ve;
   };
@@ -432,11 +443,13 @@ void attn_cache_kernel(
       const uint32_t bytes = (uint32_t)t.valid[hf] * D * ESZ;
       const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(static_cast<const char*>(cv.k) + row * (D * ESZ), bytes);
       const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(static_cast<const char*>(cv.v) + row * (D * ESZ), bytes);
+      if constexpr (!KLDS) {
 #pragma unroll
-      for (int i = 0; i < KL; ++i)
-        t.h[hf].k[i] = __builtin_bit_cast(
-            u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0,
-                                                           NT ? kNonTemporal : 0));
+        for (int i = 0; i < KL; ++i)
+          t.h[hf].k[i] = __builtin_bit_cast(
+              u32x4d, __builtin_amdgcn_raw_buffer_load_b128(rk, col * D * ESZ + 64 * i + 16 * grp, 0,
+                                                             NT ? kNonTemporal : 0));
+      }
       ca_load_c<F8, 1>(cv, p, hk, slot, rows.c_off, col, grp, &t.h[hf].c, t.h[hf].ke, t.h[hf].ve);
       // V: place s of the tile holds piece (s % CPR) ^ swizzle of key s / CPR
 #pragma unroll
@@ -444,10 +457,17 @@ void attn_cache_kernel(
         const int s = i * 64 + lane, kr = s / CPR;
         const int piece = (s % CPR) ^ v_swizzle<D, F8>(16 * hf + kr);
         ca_dma16<NT>(rv, vbuf + (hf * (VL / 2) + i) * 1024, (uint32_t)(kr * D * ESZ + 16 * piece));
+        if constexpr (KLDS)
+          ca_dma16<NT>(rk, vbuf + VBYTES + (hf * (VL / 2) + i) * 1024,
+                       (uint32_t)(kr * D * ESZ + 16 * ((s % CPR) ^ k_swizzle<D, F8>(kr))));
       }
     }
   };
 
+  const lds_byte* kat[KL];  // KLDS: this lane's pieces of its key
+#pragma unroll
+  for (int i = 0; i < KL; ++i)
+    kat[i] = lds_ptr(vbuf) + VBYTES + col * D * ESZ + 16 * ((4 * i + grp) ^ k_swizzle<D, F8>(col));
   // byte address in the V tile of this lane's transposing read for dims 0..15
   const char* vread[2];
   if constexpr (F8) {
@@ -501,9 +521,15 @@ void attn_cache_kernel(
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       s[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+      u32x4d kw[KL];
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        if constexpr (KLDS) kw[i] = __builtin_bit_cast(u32x4d, *(const lds_f32x4_t*)(kat[i] + hf * 16 * D * ESZ));
+        else kw[i] = cur.h[hf].k[i];
+      }
 #pragma unroll
       for (int st = 0; st < NS; ++st)
-        s[hf] = mfma16(k_operand<F8>(cur.h[hf].k, st, e4m3_scale(cur.h[hf].ke)), rows.q[0][st], s[hf]);
+        s[hf] = mfma16(k_operand<F8>(kw, st, e4m3_scale(cur.h[hf].ke)), rows.q[0][st], s[hf]);
     }
     const bool plain = cur.valid[0] == 16 && cur.valid[1] == 16 && key0 + kCaTile <= len;
     bf16x8 pb;
@@ -592,14 +618,6 @@ void attn_cache_kernel(
 // rows are its own, so nothing is merged at the end.
 // ---------------------------------------------------------------------------
 constexpr int kCrTile = 64;
-
-// Place of a 16-byte piece of K in its row: the 16 keys of a half whose pieces one operand
-// read touches lie in different banks.
-template <int D, bool F8>
-__device__ __forceinline__ int k_swizzle(int key) {
-  constexpr int BYTES = D * (F8 ? 1 : 2);
-  return BYTES == 256 ? key & 15 : BYTES == 128 ? (key >> 1) & 7 : (key >> 2) & 3;
-}
 
 // transposing read of 8-bit elements at a byte address, as ds_read_tr_asm; valid after
 // lds_wait8()
@@ -912,32 +930,31 @@ __global__ __launch_bounds__(D / 4 * SG) void attn_cache_join_kernel(
 // ---------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------
-// Which kernel.  The one whose waves split the keys reads K without a detour and has more of
-// them in flight; the one that shares tiles reads and converts them once for 64 or 128 rows.
-// us at 32 sequences of 8000 tokens, H_kv = 4, split / shared: bf16, d = 128 4 rows 103 / 99,
-// 24 rows 132 / 105; d = 64 16 rows 49 / 53, 24 rows 60 / 55; e4m3, d = 128 32 rows 74 / 82, 40
-// rows 95 / 82; d = 64 32 rows 40 / 66, 64 rows 63 / 66; a single sequence of 2000, 4 rows 10.6 / 12.1.
+// Which kernel.  The one whose waves split the keys starts and ends faster; the one that shares
+// tiles reads and converts them once for 64 or 128 rows.  us at 32 sequences of 8000 tokens, H_kv =
+// 4, split / shared: bf16, d = 128 4 rows 93.6 / 88.8, 24 rows 132 / 93; d = 64 16 rows 49.1 / 49.4, 24
+// rows 55 / 51; e4m3, d = 128 32 rows 71 / 74, 40 rows 87 / 75; d = 64 32 rows 39 / 62, 64 rows 61 / 66;
+// a single bf16 sequence of 2000, d = 128, 4 rows 10.6 / 12.0.
 // Two row tiles to a wave halve the tiles' reads and conversions but need twice the rows: 128
-// rows, H_kv = 2, d = 128 two / one e4m3 67 / 78, bf16 72 / 78, but one sequence of 2000 with
-// H_kv = 4 19.3 / 15.7 and 18.0 / 14.1, one of 16000 27.5 / 26.9 and 24.5 / 22.8.
+// rows, d = 128 two / one, 32 sequences of 8000, H_kv = 2 e4m3 71 / 78, bf16 74 / 78, but one of 2000
+// with H_kv = 4 19.4 / 15.6 and 18.0 / 14.0, one of 16000 27.1 / 26.0 and 23.7 / 22.0.
 constexpr long long kCrTwo = 1 << 17;  // keys of all workgroups from which two row tiles pay
 // How many workgroups the keys are split for.  Sharing: as many as are resident, two or
-// three to a CU (512 / 768 / 1024 workgroups: e4m3, one row tile 90 / 82 / 87 us; bf16, d = 128 119 /
-// 131 / 124; two row tiles, 64 drafts of four sequences, 54 / 64 / 68).  Splitting waves: far more,
-// so that sequences of different lengths even out (512 / 1024 / 2048 / 4096: 64 sequences of
-// 8 to 32 thousand tokens 286 / 264 / 260 / 259 us).
+// three to a CU (512 / 768 / 1024 workgroups, 64 rows: e4m3, one row tile 88 / 80 / 85 us; bf16,
+// d = 128 99 / 121 / 111; two row tiles 54 / 62 / 61).  Splitting waves: far more, so that sequences
+// of different lengths even out (512 / 1024 / 2048 / 4096: 64 sequences of 8 to 32 thousand
+// tokens 250 / 228 / 225 / 226 us).
 constexpr long long kCaWant = 2048, kCrWant2 = 512, kCrWant3 = 768;
 // The least keys of a piece, 256, 512 or 1024, by the keys of all workgroups: small calls want
 // short pieces, larger ones fewer to start and to join.  256 / 512 / 1024, H_kv = 4, e4m3, d = 128:
-// one sequence of 2000 9.8 / 11.8 / 15.5 us; one of 30000 17.7 / 15.9 / 19.0; 32 of 2000 22.4 / 19.4 /
-// 20.2; 128 of 1000 36.9 / 33.0 / 26.3 (not split).  Sharing, 1024 leaves CUs idle where the
+// one sequence of 2000 9.3 / 10.8 / 13.7 us; one of 30000 17.5 / 14.9 / 17.1; 32 of 2000 22.1 / 19.3 /
+// 19.0; 128 of 1000 37.4 / 32.4 / 26.3 (not split).  Sharing, 1024 leaves CUs idle where the
 // lengths differ: 64 drafts of four sequences of 3 to 16 thousand tokens 51 / 51 / 66.
 constexpr long long kCaSome = 80000, kCaMany = 500000;
-
 // Bytes of K and V from which they bypass the caches when one row block reads them: 1.5 times
 // the 256 MB that the last level holds.  us with / without: e4m3, d = 128, 64 sequences of 20000
-// (1.3 GB) 237 / 257, 32 of 8000 (262 MB, in the cache from the call before) 60 / 53; bf16 64 of
-// 20000 430 / 477, 32 of 8000 95 / 103.
+// (1.3 GB) 213 / 248, 32 of 8000 (262 MB, in the cache from the call before) 56 / 51; bf16 64 of
+// 20000 425 / 462, 32 of 8000 97 / 106.
 constexpr long long kCaBypass = 384LL << 20;
 
 struct CaPlan {
@@ -950,12 +967,13 @@ static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
   CaPlan p;
   const int rows = s.H / s.Hkv * n;
   const long long seqs = (long long)s.B * s.Hkv;
-  p.shared = rows > (s.f8 ? (s.d == 64 ? 64 : 32) : 16);
+  const bool large = seqs * max_len * 2 * s.d * (s.f8 ? 1 : 2) >= kCaBypass;
+  p.shared = rows > (s.f8 ? (s.d == 64 ? 64 : 32) : large && s.d == 128 ? 0 : 16);
   auto blocks = [&](int rt) { return (rows + 64 * rt - 1) / (64 * rt); };
   p.rt = p.shared && rows > 64 && seqs * blocks(2) * max_len >= kCrTwo ? 2 : 1;
   p.n_rowblk = p.shared ? blocks(p.rt) : (rows + 15) / 16;
   const long long all = seqs * p.n_rowblk * max_len;  // keys of all workgroups, at most
-  p.once = p.n_rowblk == 1 && all * 2 * s.d * (s.f8 ? 1 : 2) >= kCaBypass;
+  p.once = p.n_rowblk == 1 && large;
   const int least = all < kCaSome ? 256 : all < kCaMany || p.shared ? 512 : 1024;
   const long long want = !p.shared ? kCaWant : p.rt == 2 || (s.d == 128 && !s.f8) ? kCrWant2 : kCrWant3;
   p.split.unit = p.shared ? kCrTile : kCaRound;
@@ -991,19 +1009,21 @@ hipError_t launch_attn_cache(const CacheSpec& s, const void* q, const int* seq_l
   }
   const unsigned nbase = (unsigned)s.Hkv * p.n_pieces;
   const dim3 grid((nbase + 7) / 8 * 8 * (unsigned)p.n_rowblk);
-  auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kCaThreads), 0, st, cache_view(s), (const bf16*)q, seq_len,
+  auto run = [&](auto kernel, auto once) {
+    hipLaunchKernelGGL(p.once ? once : kernel, grid, dim3(kCaThreads), 0, st, cache_view(s), (const bf16*)q, seq_len,
                        parent, n_new, (bf16*)o, lse, parts, p.split, n, s.H / s.Hkv, p.n_rowblk,
                        p.n_pieces, scale * kLog2e);
   };
   auto by_rows = [&](auto dc, auto f8) {
     constexpr int D = decltype(dc)::value;
     constexpr bool F8 = decltype(f8)::value;
-    if (p.rt == 2) run(attn_cache_rows_kernel<D, F8, 2, false>);
-    else if (p.shared && p.once) run(attn_cache_rows_kernel<D, F8, 1, true>);
-    else if (p.shared) run(attn_cache_rows_kernel<D, F8, 1, false>);
-    else if (p.once) run(attn_cache_kernel<D, F8, true>);
-    else run(attn_cache_kernel<D, F8, false>);
+    // what ca_plan never asks for: large bf16 caches, d = 128, are always shared, and e4m3, d = 64,
+    // is shared from 65 rows on, with two row tiles if it is large
+    constexpr bool SPLIT_ONCE = F8 || D == 64, SHARE_ONCE = !F8 || D == 128;
+    if (p.rt == 2) run(attn_cache_rows_kernel<D, F8, 2, false>, attn_cache_rows_kernel<D, F8, 2, false>);
+    else if (p.shared) run(attn_cache_rows_kernel<D, F8, 1, false>,
+                           attn_cache_rows_kernel<D, F8, 1, SHARE_ONCE>);
+    else run(attn_cache_kernel<D, F8, false>, attn_cache_kernel<D, F8, SPLIT_ONCE>);
   };
   auto by_format = [&](auto dc) {
     if (s.f8) by_rows(dc, std::true_type());
