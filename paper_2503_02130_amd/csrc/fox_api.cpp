@@ -951,7 +951,7 @@ fox_status_t fox_attn_cache(const fox_cache_t* cache, const void* q, const int* 
 }
 
 size_t fox_packed_plan_bytes(int B, int N) {
-  return B <= 0 || N <= 0 ? 0 : (size_t)fox::packed_items(B, N) * 16;
+  return check_packed(B, 1, 1, N) ? 0 : (size_t)fox::packed_items(B, N) * 16;
 }
 
 fox_status_t fox_packed_plan(const int* cu_seqlens, int B, int N, void* plan, size_t plan_bytes,

@@ -122,6 +122,7 @@ def test_packed_arguments(lib):
     p = P16
     assert lib.fox_packed_plan_bytes(0, 10) == 0 and lib.fox_packed_plan_bytes(3, 0) == 0
     assert lib.fox_packed_plan_bytes(3, 1000) == 16 * (7 + 3)
+    assert lib.fox_packed_plan_bytes(2 ** 31 - 1, 2 ** 31 - 1) == 0
     plan = lib.fox_packed_plan
     assert plan(None, 1, 10, p, 1 << 20, None, 0, None) == NULL
     assert plan(p, 0, 10, p, 1 << 20, None, 0, None) == SHAPE
