@@ -584,7 +584,8 @@ fox_status_t fox_packed_zero_behind(const fox_packed_rows_t* tensors, int n, con
  *   format      FOX_CACHE_BF16, or FOX_CACHE_E4M3: each row of d codes with one scale, a
  *               power of two 2^(exp - 127) chosen from the row's largest magnitude (the
  *               least that brings it to 448 or below, from 2^-126), so that every value is
- *               the nearest code times the scale, ties to even, and exact in bf16
+ *               the nearest code times the scale, ties to even, and exact in bf16 (magnitudes
+ *               above 3.29e38 may round to infinity)
  *   k, v        [n_pages, H_kv, page, d]  of the format's type
  *   k_exp,v_exp [n_pages, H_kv, page]     uint8, the rows' exp (E4M3 only, else NULL)
  *   c           [n_pages, H, page]        fp32, the running sum of log f
