@@ -778,8 +778,8 @@ static void packed_bwd_f32_t(const float* q, const float* k, const float* v, con
 hipError_t launch_packed_bwd_f32(const float* q, const float* k, const float* v, const float* c,
                                  const float* o, const float* lse, const float* d_o, float* dq,
                                  float* dk, float* dv, float* delta, float* dcq, float* dck,
-                                 float* part, const void* plan, const int* cu, int B, int H,
-                                 int Hkv, int N, int d, int max_len, float scale, hipStream_t s) {
+                                 float* part, const void* plan, int B, int H, int Hkv, int N,
+                                 int d, int max_len, float scale, hipStream_t s) {
   const hipError_t e = launch_bwd_delta(false, o, d_o, delta, H, N, d, s);
   if (e != hipSuccess) return e;
   const int splits = packed_head_split(false, H, Hkv, N, d, max_len);
@@ -788,7 +788,6 @@ hipError_t launch_packed_bwd_f32(const float* q, const float* k, const float* v,
     packed_bwd_f32_t<128, 4>(q, k, v, c, lse, d_o, delta, dq, dk, dv, dcq, dck, pk, scale, s);
   else
     packed_bwd_f32_t<64, 8>(q, k, v, c, lse, d_o, delta, dq, dk, dv, dcq, dck, pk, scale, s);
-  if (splits > 1) return launch_packed_head_sum(false, part, cu, dk, dv, B, Hkv, N, d, splits, s);
   return hipGetLastError();
 }
 

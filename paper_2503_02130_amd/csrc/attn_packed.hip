@@ -1028,44 +1028,6 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   }
 }
 
-// dK and dV from the partial sums of `splits` groups of heads, in the order of the groups; rows
-// behind the last sequence (no partial sums) are left as they were.
-template <typename T>
-__global__ __launch_bounds__(256) void packed_head_sum_kernel(const float* __restrict__ part,
-                                                              const int* __restrict__ cu,
-                                                              T* __restrict__ dK, T* __restrict__ dV,
-                                                              int B, int Hkv, int N, int d,
-                                                              int splits) {
-  const size_t n4 = (size_t)Hkv * N * d / 4;  // pieces of four of one tensor
-  const int end = min(max(cu[B], 0), N);
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < 2 * n4; i += (size_t)gridDim.x * 256) {
-    const size_t at = i < n4 ? i : i - n4;
-    if ((int)(at / (d / 4) % N) >= end) continue;
-    f32x4 sum = reinterpret_cast<const f32x4*>(part)[i];
-    for (int s = 1; s < splits; ++s) sum += reinterpret_cast<const f32x4*>(part)[(size_t)s * 2 * n4 + i];
-    T* out = (i < n4 ? dK : dV) + 4 * at;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<bf16x4*>(out) =
-          bf16x4{to_bf16(sum[0]), to_bf16(sum[1]), to_bf16(sum[2]), to_bf16(sum[3])};
-    } else {
-      *reinterpret_cast<f32x4*>(out) = sum;
-    }
-  }
-}
-
-hipError_t launch_packed_head_sum(bool bf16_, const float* part, const int* cu, void* dk, void* dv,
-                                  int B, int Hkv, int N, int d, int splits, hipStream_t s) {
-  const size_t n = (size_t)Hkv * N * d / 2;
-  const dim3 grid((unsigned)std::min<size_t>((n + 255) / 256, 4096));
-  if (bf16_)
-    hipLaunchKernelGGL(packed_head_sum_kernel<bf16>, grid, dim3(256), 0, s, part, cu, (bf16*)dk,
-                       (bf16*)dv, B, Hkv, N, d, splits);
-  else
-    hipLaunchKernelGGL(packed_head_sum_kernel<float>, grid, dim3(256), 0, s, part, cu, (float*)dk,
-                       (float*)dv, B, Hkv, N, d, splits);
-  return hipGetLastError();
-}
-
 // Groups that the query heads of a key head are split into for dK and dV, a divisor of G.  A
 // workgroup walks G / groups heads times the query tiles behind its keys, so the time is about
 // the larger of the longest sequence's walk and the mean load of the part, and each split
@@ -1138,8 +1100,8 @@ hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const 
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
                              const void* o, const void* o_lo, const float* lse, const void* d_o,
                              void* dq, void* dk, void* dv, float* delta, float* dck, float* part,
-                             const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
-                             int max_len, float scale, hipStream_t s) {
+                             const void* plan, int B, int H, int Hkv, int N, int d, int max_len,
+                             float scale, hipStream_t s) {
   const unsigned items = (unsigned)packed_items(B, N);
   const int splits = packed_head_split(true, H, Hkv, N, d, max_len);
   auto kv = [&](auto kernel) {
@@ -1163,7 +1125,6 @@ hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const 
     else qs(packed_dq_kernel<64, 1>, 1);
     kv(packed_dkdv_kernel<64, 32>);
   }
-  if (splits > 1) return launch_packed_head_sum(true, part, cu, dk, dv, B, Hkv, N, d, splits, s);
   return hipGetLastError();
 }
 

@@ -1037,22 +1037,24 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
   hipError_t e;
   if (dtype == FOX_DTYPE_BF16)
     e = fox::launch_packed_bwd(q, k, v, c, o, o_lo, lse, d_o, dq, dk, dv, delta, dck, part, plan,
-                               cu_seqlens, B, H, H_kv, N, d, len, scale, stream);
+                               B, H, H_kv, N, d, len, scale, stream);
   else
     e = fox::launch_packed_bwd_f32((const float*)q, (const float*)k, (const float*)v, c,
                                    (const float*)o, lse, (const float*)d_o, (float*)dq, (float*)dk,
-                                   (float*)dv, delta, dcq, dck, part, plan, cu_seqlens, B, H,
-                                   H_kv, N, d, len, scale, stream);
+                                   (float*)dv, delta, dcq, dck, part, plan, B, H, H_kv, N, d,
+                                   len, scale, stream);
   const int esz = dtype == FOX_DTYPE_BF16 ? 2 : 4;
   const fox::ZeroRows zeros[] = {{dq, H, d * esz},
                                  {dk, H_kv, d * esz},
                                  {dv, H_kv, d * esz},
                                  {d_logit, H, gate_dtype == FOX_DTYPE_BF16 ? 2 : 4},
                                  {d_log_f, H, 4}};
+  const bool bf = dtype == FOX_DTYPE_BF16;
+  const fox::HeadSum sum{part, dk, dv, bf, fox::packed_head_split(bf, H, H_kv, N, d, len), H_kv, d};
   if (e == hipSuccess)
     e = fox::launch_packed_gate_grad(gate_dtype == FOX_DTYPE_BF16,
                                      dtype == FOX_DTYPE_BF16 ? nullptr : dcq, dck, gate_logit,
-                                     cu_seqlens, d_log_f, d_logit, B, H, N, zeros,
+                                     cu_seqlens, d_log_f, d_logit, B, H, N, sum, zeros,
                                      !zero_behind ? 0 : d_log_f ? 5 : 4, stream);
   return launch_status(e);
 }

@@ -226,31 +226,36 @@ hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, const Zer
                               int n_zeros, hipStream_t s);
 hipError_t launch_packed_prefix(bool bf16, const void* logit, const int* cu, float* c, int B,
                                 int H, int N, hipStream_t s);
-hipError_t launch_packed_gate_grad(bool bf16, const float* dcq, const float* dck,
-                                   const void* logit, const int* cu, float* d_log_f,
-                                   void* d_logit, int B, int H, int N, const ZeroRows* zeros,
-                                   int n_zeros, hipStream_t s);
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
                              void* o_lo, float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s);
 // Groups that the query heads of a key head are split into for dK and dV; with more than one,
-// `part` holds their partial sums, fp32 [groups][2][Hkv][N][d].
+// dk and dv are partial sums, fp32 [groups][2][Hkv][N][d], which the gate gradient's launch adds
+// up in the order of the groups.
 int packed_head_split(bool bf16, int H, int Hkv, int N, int d, int max_len);
-hipError_t launch_packed_head_sum(bool bf16, const float* part, const int* cu, void* dk, void* dv,
-                                  int B, int Hkv, int N, int d, int splits, hipStream_t s);
+struct HeadSum {
+  const float* part;
+  void* dk;
+  void* dv;
+  int bf16, splits, Hkv, d;
+};
+hipError_t launch_packed_gate_grad(bool bf16, const float* dcq, const float* dck,
+                                   const void* logit, const int* cu, float* d_log_f,
+                                   void* d_logit, int B, int H, int N, const HeadSum& sum,
+                                   const ZeroRows* zeros, int n_zeros, hipStream_t s);
 // dq, dk, dv and dc_k (delta: [H, N] scratch); in bf16 dc_q is 0, in fp32 it is given too
 hipError_t launch_packed_bwd(const void* q, const void* k, const void* v, const float* c,
                              const void* o, const void* o_lo, const float* lse, const void* d_o,
                              void* dq, void* dk, void* dv, float* delta, float* dck, float* part,
-                             const void* plan, const int* cu, int B, int H, int Hkv, int N, int d,
-                             int max_len, float scale, hipStream_t s);
+                             const void* plan, int B, int H, int Hkv, int N, int d, int max_len,
+                             float scale, hipStream_t s);
 hipError_t launch_packed_fwd_f32(const float* q, const float* k, const float* v, const float* c,
                                  float* o, float* lse, const void* plan, int B, int H, int Hkv,
                                  int N, int d, float scale, hipStream_t s);
 hipError_t launch_packed_bwd_f32(const float* q, const float* k, const float* v, const float* c,
                                  const float* o, const float* lse, const float* d_o, float* dq,
                                  float* dk, float* dv, float* delta, float* dcq, float* dck,
-                                 float* part, const void* plan, const int* cu, int B, int H,
-                                 int Hkv, int N, int d, int max_len, float scale, hipStream_t s);
+                                 float* part, const void* plan, int B, int H, int Hkv, int N,
+                                 int d, int max_len, float scale, hipStream_t s);
 
 }  // namespace fox

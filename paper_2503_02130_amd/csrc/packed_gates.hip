@@ -64,6 +64,31 @@ __global__ __launch_bounds__(256) void packed_zero_kernel(ZeroList list, const i
   zero_behind(list, cu, B, N, (int)blockIdx.x);
 }
 
+// dK and dV from the partial sums of groups of heads, in the order of the groups, by workgroup
+// `group` of kSumGroups; rows behind the last sequence (no partial sums) are left as they were.
+constexpr int kSumGroups = 512;
+template <typename T>
+__device__ __forceinline__ void head_sum(const HeadSum& x, const int* __restrict__ cu, int B, int N,
+                                         int group) {
+  const size_t n4 = (size_t)x.Hkv * N * x.d / 4;  // pieces of four of one tensor
+  const int end = min(max(cu[B], 0), N);
+  for (size_t i = (size_t)group * blockDim.x + threadIdx.x; i < 2 * n4;
+       i += (size_t)kSumGroups * blockDim.x) {
+    const size_t at = i < n4 ? i : i - n4;
+    if ((int)(at / (x.d / 4) % N) >= end) continue;
+    f32x4 sum = reinterpret_cast<const f32x4*>(x.part)[i];
+    for (int s = 1; s < x.splits; ++s)
+      sum += reinterpret_cast<const f32x4*>(x.part)[(size_t)s * 2 * n4 + i];
+    T* out = static_cast<T*>(i < n4 ? x.dk : x.dv) + 4 * at;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<bf16x4*>(out) =
+          bf16x4{to_bf16(sum[0]), to_bf16(sum[1]), to_bf16(sum[2]), to_bf16(sum[3])};
+    } else {
+      *reinterpret_cast<f32x4*>(out) = sum;
+    }
+  }
+}
+
 __global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict__ cu, int B, int N,
                                                           PackedItem* __restrict__ items,
                                                           int n_items, int plan_groups,
@@ -130,8 +155,14 @@ template <bool GRAD, typename T>
 __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
     const float* __restrict__ dcq, const float* __restrict__ dck, const T* __restrict__ logit,
     const int* __restrict__ cu, float* __restrict__ c, float* __restrict__ aux,
-    T* __restrict__ d_logit, int B, int H, int N, ZeroList zeros) {
-  if (GRAD && (int)blockIdx.x >= B * H) return zero_behind(zeros, cu, B, N, (int)blockIdx.x - B * H);
+    T* __restrict__ d_logit, int B, int H, int N, ZeroList zeros, HeadSum heads) {
+  if (GRAD && (int)blockIdx.x >= B * H) {  // what rides on the launch: heads' sums, then zeros
+    const int other = (int)blockIdx.x - B * H, sums = heads.splits > 1 ? kSumGroups : 0;
+    if (other >= sums) zero_behind(zeros, cu, B, N, other - sums);
+    else if (heads.bf16) head_sum<bf16>(heads, cu, B, N, other);
+    else head_sum<float>(heads, cu, B, N, other);
+    return;
+  }
   __shared__ __attribute__((aligned(16))) float row[kPScanSegment];
   __shared__ double wave_total[kPScanThreads / 64];
   const int b = (int)(blockIdx.x / H), h = (int)(blockIdx.x % H);
@@ -231,26 +262,28 @@ hipError_t launch_packed_prefix(bool bf16_, const void* logit, const int* cu, fl
   const dim3 grid((unsigned)B * (unsigned)H), block(kPScanThreads);
   if (bf16_)
     hipLaunchKernelGGL((packed_scan_kernel<false, bf16>), grid, block, 0, s, nullptr, nullptr,
-                       (const bf16*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{});
+                       (const bf16*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{}, HeadSum{});
   else
     hipLaunchKernelGGL((packed_scan_kernel<false, float>), grid, block, 0, s, nullptr, nullptr,
-                       (const float*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{});
+                       (const float*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{}, HeadSum{});
   return hipGetLastError();
 }
 
 hipError_t launch_packed_gate_grad(bool bf16_, const float* dcq, const float* dck,
                                    const void* logit, const int* cu, float* d_log_f,
-                                   void* d_logit, int B, int H, int N, const ZeroRows* zeros,
-                                   int n_zeros, hipStream_t s) {
-  const dim3 grid((unsigned)B * (unsigned)H + (n_zeros ? kZeroGroups : 0)), block(kPScanThreads);
+                                   void* d_logit, int B, int H, int N, const HeadSum& sum,
+                                   const ZeroRows* zeros, int n_zeros, hipStream_t s) {
+  const dim3 grid((unsigned)B * (unsigned)H + (sum.splits > 1 ? kSumGroups : 0) +
+                  (n_zeros ? kZeroGroups : 0)),
+      block(kPScanThreads);
   if (bf16_)
     hipLaunchKernelGGL((packed_scan_kernel<true, bf16>), grid, block, 0, s, dcq, dck,
                        (const bf16*)logit, cu, nullptr, d_log_f, (bf16*)d_logit, B, H, N,
-                       zero_list(zeros, n_zeros));
+                       zero_list(zeros, n_zeros), sum);
   else
     hipLaunchKernelGGL((packed_scan_kernel<true, float>), grid, block, 0, s, dcq, dck,
                        (const float*)logit, cu, nullptr, d_log_f, (float*)d_logit, B, H, N,
-                       zero_list(zeros, n_zeros));
+                       zero_list(zeros, n_zeros), sum);
   return hipGetLastError();
 }
 
