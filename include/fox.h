@@ -537,6 +537,7 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  *   NULL).  Blocks of a list that do not lie within a call's N rows are skipped.
  * fox_gate_prefix_packed: c, the running sum of log sigmoid(gate_logit) within each sequence
  *   (summed in 64 bits, rounded once).
+ * fox_packed_start: fox_packed_plan and fox_gate_prefix_packed in one launch.
  * fox_attn_fwd_packed: O and LSE of each sequence as fox_attn_fwd's.  max_len: the longest
  *   sequence, if known, else 0 (N): it decides how the work is split, not what is computed.
  *   o_lo (bf16, may be NULL): what rounding took from o, for the backward.
@@ -562,6 +563,9 @@ fox_status_t fox_packed_plan(const int* cu_seqlens, int B, int N, void* plan, si
 fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_logit,
                            const int* cu_seqlens, float* c, int B, int H, int N,
                            hipStream_t stream);
+fox_status_t fox_packed_start(fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
+                     float* c, int B, int H, int N, void* plan, size_t plan_bytes,
+                     const fox_packed_rows_t* tensors, int n, hipStream_t stream);
 fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,
                         const float* c, const void* plan, void* o, void* o_lo, float* lse, int B, int H,
                         int H_kv, int N, int d, int max_len, float scale, hipStream_t stream);

@@ -31,7 +31,7 @@ from ._cache import (  # noqa: E402,F401
     fox_attn_cache, fox_attn_cache_workspace_bytes,
 )
 from ._packed import (  # noqa: E402,F401
-    fox_packed_plan, fox_gate_prefix_packed, fox_attn_fwd_packed, fox_attn_bwd_packed,
+    fox_packed_plan, fox_gate_prefix_packed, fox_packed_start, fox_attn_fwd_packed, fox_attn_bwd_packed,
     fox_attn_bwd_packed_workspace_bytes, fox_packed_zero_behind,
 )
 from .autograd import (  # noqa: E402,F401
@@ -62,7 +62,7 @@ __all__ = [
     "fox_gate_projection", "fox_gate_projection_bwd", "fox_gate_projection_bwd_workspace_bytes",
     "PagedCache", "fox_cache_append", "fox_cache_append_packed", "fox_cache_keep",
     "fox_cache_read", "fox_attn_cache", "fox_attn_cache_workspace_bytes",
-    "PackedForgettingAttention", "forgetting_attention_packed", "fox_packed_plan",
+    "PackedForgettingAttention", "forgetting_attention_packed", "fox_packed_plan", "fox_packed_start",
     "fox_gate_prefix_packed", "fox_attn_fwd_packed", "fox_attn_bwd_packed",
     "fox_attn_bwd_packed_workspace_bytes", "fox_packed_zero_behind",
 ]

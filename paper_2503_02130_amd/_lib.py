@@ -42,7 +42,8 @@ EXPORTED = (
     "fox_gate_projection", "fox_gate_projection_bwd_workspace_bytes", "fox_gate_projection_bwd",
     "fox_cache_append", "fox_cache_append_packed", "fox_cache_keep", "fox_cache_read",
     "fox_attn_cache_workspace_bytes", "fox_attn_cache",
-    "fox_packed_plan_bytes", "fox_packed_plan", "fox_gate_prefix_packed", "fox_attn_fwd_packed",
+    "fox_packed_plan_bytes", "fox_packed_plan", "fox_gate_prefix_packed",
+    "fox_packed_start", "fox_attn_fwd_packed",
     "fox_attn_bwd_packed_workspace_bytes", "fox_attn_bwd_packed", "fox_packed_zero_behind",
 )
 
@@ -177,6 +178,7 @@ def load() -> ctypes.CDLL:
             ("fox_attn_cache", [P, P, P, P, P, P, P, P, Z, I, I, F, P]),
             ("fox_packed_plan", [P, I, I, P, Z, P, I, P]),
             ("fox_gate_prefix_packed", [I, P, P, P, I, I, I, P]),
+            ("fox_packed_start", [I, P, P, P, I, I, I, P, Z, P, I, P]),
             ("fox_attn_fwd_packed", [I, P, P, P, P, P, P, P, P, I, I, I, I, I, I, F, P]),
             ("fox_attn_bwd_packed", [I, P, P, P, P, P, P, P, P, I, P, P, P, P, P, P, P, P, I, P, Z,
                                      I, I, I, I, I, I, F, P]),

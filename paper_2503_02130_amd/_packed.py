@@ -78,6 +78,24 @@ def fox_gate_prefix_packed(gate_logit: torch.Tensor, cu_seqlens: torch.Tensor,
     return c
 
 
+def fox_packed_start(gate_logit: torch.Tensor, cu_seqlens: torch.Tensor
+                     ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(plan, c): fox_packed_plan and fox_gate_prefix_packed in one launch."""
+    H, N = gate_logit.shape
+    dt, dev = gate_logit.dtype, gate_logit.device
+    if dt not in _DT:
+        raise ValueError(f"unsupported dtype {dt}")
+    _check(gate_logit, "gate_logit", (H, N), dt, None)
+    B = _check_cu(cu_seqlens, dev)
+    places = _plan_places(B, N)
+    plan = torch.empty((places * 4,), device=dev, dtype=torch.int32)
+    c = torch.empty((H, N), device=dev, dtype=torch.float32)
+    st = _call(load().fox_packed_start, dev, _DT[dt], _ptr(gate_logit), _ptr(cu_seqlens), _ptr(c), B,
+               H, N, _ptr(plan), 16 * places, None, 0)
+    _raise(st, "fox_packed_start")
+    return plan, c
+
+
 def fox_attn_fwd_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c: torch.Tensor,
                         cu_seqlens: torch.Tensor, plan: Optional[torch.Tensor] = None,
                         max_len: int = 0, scale: Optional[float] = None,
@@ -201,14 +219,14 @@ def _step_forward(q, k, v, gate_logit, cu_seqlens, plan, max_len, scale):
     if plan is None:
         places = _plan_places(B, N)
         plan = torch.empty((places * 4,), device=dev, dtype=torch.int32)
-        _raise(_call(lib.fox_packed_plan, dev, cu, B, N, _ptr(plan), 16 * places,
-                     ctypes.addressof(row), 1), "fox_packed_plan")
+        _raise(_call(lib.fox_packed_start, dev, _DT[gdt], _ptr(gate_logit), cu, _ptr(c), B, H, N,
+                     _ptr(plan), 16 * places, ctypes.addressof(row), 1), "fox_packed_start")
     else:
         _check_plan(plan, B, N, dev)
         _raise(_call(lib.fox_packed_zero_behind, dev, ctypes.addressof(row), 1, cu, B, N),
                "fox_packed_zero_behind")
-    _raise(_call(lib.fox_gate_prefix_packed, dev, _DT[gdt], _ptr(gate_logit), cu, _ptr(c), B, H, N),
-           "fox_gate_prefix_packed")
+        _raise(_call(lib.fox_gate_prefix_packed, dev, _DT[gdt], _ptr(gate_logit), cu, _ptr(c), B, H,
+                     N), "fox_gate_prefix_packed")
     _raise(_call(lib.fox_attn_fwd_packed, dev, dt, _ptr(q), _ptr(k), _ptr(v), _ptr(c), _ptr(plan),
                  _ptr(o), _ptr(o_lo), _ptr(lse), B, H, Hkv, N, d, max_len, scale),
            "fox_attn_fwd_packed")

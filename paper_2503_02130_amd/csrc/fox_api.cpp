@@ -976,7 +976,24 @@ fox_status_t fox_gate_prefix_packed(fox_dtype_t gate_dtype, const void* gate_log
   if (!cache_dtype(gate_dtype)) return FOX_ERR_UNSUPPORTED;
   if (!all_aligned16({gate_logit, cu_seqlens, c})) return FOX_ERR_ALIGN;
   return launch_status(fox::launch_packed_prefix(gate_dtype == FOX_DTYPE_BF16, gate_logit,
-                                                 cu_seqlens, c, B, H, N, stream));
+                                                 cu_seqlens, c, B, H, N, nullptr, nullptr, 0,
+                                                 stream));
+}
+
+fox_status_t fox_packed_start(fox_dtype_t gate_dtype, const void* gate_logit, const int* cu_seqlens,
+                     float* c, int B, int H, int N, void* plan, size_t plan_bytes,
+                     const fox_packed_rows_t* tensors, int n, hipStream_t stream) {
+  if (!all_set({gate_logit, cu_seqlens, c, plan})) return FOX_ERR_NULL;
+  fox_status_t st = check_packed(B, H, H, N);
+  if (st) return st;
+  if (!cache_dtype(gate_dtype)) return FOX_ERR_UNSUPPORTED;
+  if (!all_aligned16({gate_logit, cu_seqlens, c, plan})) return FOX_ERR_ALIGN;
+  if (plan_bytes < fox_packed_plan_bytes(B, N)) return FOX_ERR_WORKSPACE;
+  fox::ZeroRows x[fox::kZeroTensors];
+  st = zero_rows(tensors, n, x);
+  if (st) return st;
+  return launch_status(fox::launch_packed_prefix(gate_dtype == FOX_DTYPE_BF16, gate_logit,
+                                                 cu_seqlens, c, B, H, N, plan, x, n, stream));
 }
 
 fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k, const void* v,

@@ -224,8 +224,10 @@ hipError_t launch_packed_zero(const ZeroRows* x, int n, const int* cu, int B, in
                               hipStream_t s);
 hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, const ZeroRows* zeros,
                               int n_zeros, hipStream_t s);
+// c and, with a plan, the list (then the zeros too) in the same launch
 hipError_t launch_packed_prefix(bool bf16, const void* logit, const int* cu, float* c, int B,
-                                int H, int N, hipStream_t s);
+                                int H, int N, void* plan, const ZeroRows* zeros, int n_zeros,
+                                hipStream_t s);
 hipError_t launch_packed_fwd(const void* q, const void* k, const void* v, const float* c, void* o,
                              void* o_lo, float* lse, const void* plan, int B, int H, int Hkv, int N, int d,
                              int max_len, float scale, hipStream_t s);

@@ -13,7 +13,9 @@
 // The scans run in 64 bits and round once: c of a long sequence is thousands with
 // differences of neighbours that matter, and fp32 sums of it are several units off.  They
 // are short chains of a few barriers per 8192 rows, bound by latency: sequences of up to 8191
-// rows take 6 us, their gradient 12, the plan 4.
+// rows take 6 us, their gradient 12, the plan 4.  What does not depend on a scan rides on its
+// launch: the plan on the prefix's, the sums of split heads (24 us alone beside these 12: 27
+// together) and the zeros behind the last sequence on the gradient's.
 #include <algorithm>
 
 #include "fox_internal.h"
@@ -89,14 +91,16 @@ __device__ __forceinline__ void head_sum(const HeadSum& x, const int* __restrict
   }
 }
 
-__global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict__ cu, int B, int N,
-                                                          PackedItem* __restrict__ items,
-                                                          int n_items, int plan_groups,
-                                                          ZeroList zeros) {
-  if ((int)blockIdx.x >= plan_groups)
-    return zero_behind(zeros, cu, B, N, (int)blockIdx.x - plan_groups);
+int packed_items(int B, int N) { return N / kPackedBlock + std::min(B, N); }
+
+// The list's places of block number m, by one wave.
+struct PlanOut {
+  PackedItem* items;
+  int n_items, groups;  // workgroups that make it
+};
+__device__ __forceinline__ void make_plan(const PlanOut& plan, const int* __restrict__ cu, int B, int N,
+                                          int m) {
   const int lane = threadIdx.x & 63;
-  const int m = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
   long long before = 0, total = 0;
   for (int s = lane; s < B; s += 64) {
     int start, len;
@@ -116,11 +120,28 @@ __global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict_
     const bool has = (len + kPackedBlock - 1) / kPackedBlock > m;
     const uint64_t mask = __ballot(has);
     const long long at = before + __popcll(mask & ((1ull << lane) - 1));
-    if (has && at < n_items) items[at] = PackedItem{start, len, m, s0 + lane};
+    if (has && at < plan.n_items) plan.items[at] = PackedItem{start, len, m, s0 + lane};
     before += __popcll(mask);
   }
   if (m == 0)
-    for (long long i = total + lane; i < n_items; i += 64) items[i] = PackedItem{0, 0, 0, -1};
+    for (long long i = total + lane; i < plan.n_items; i += 64)
+      plan.items[i] = PackedItem{0, 0, 0, -1};
+}
+// Workgroup `group` of those that make the list, then of those that write zeros.
+__device__ __forceinline__ void plan_or_zeros(const PlanOut& plan, const ZeroList& zeros,
+                                              const int* __restrict__ cu, int B, int N, int group) {
+  if (group < plan.groups)
+    make_plan(plan, cu, B, N, group * (int)(blockDim.x >> 6) + (int)(threadIdx.x >> 6));
+  else
+    zero_behind(zeros, cu, B, N, group - plan.groups);
+}
+__global__ __launch_bounds__(256) void packed_plan_kernel(const int* __restrict__ cu, int B, int N,
+                                                          PlanOut plan, ZeroList zeros) {
+  plan_or_zeros(plan, zeros, cu, B, N, (int)blockIdx.x);
+}
+static PlanOut plan_out(void* plan, int B, int N, int waves) {  // a wave per block number
+  const int blocks = (N + kPackedBlock - 1) / kPackedBlock;
+  return PlanOut{(PackedItem*)plan, packed_items(B, N), (blocks + waves - 1) / waves};
 }
 
 // exp(a), a <= 0, on the transcendental unit: the product with log2(e) in two parts, so that large
@@ -155,12 +176,17 @@ template <bool GRAD, typename T>
 __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
     const float* __restrict__ dcq, const float* __restrict__ dck, const T* __restrict__ logit,
     const int* __restrict__ cu, float* __restrict__ c, float* __restrict__ aux,
-    T* __restrict__ d_logit, int B, int H, int N, ZeroList zeros, HeadSum heads) {
-  if (GRAD && (int)blockIdx.x >= B * H) {  // what rides on the launch: heads' sums, then zeros
-    const int other = (int)blockIdx.x - B * H, sums = heads.splits > 1 ? kSumGroups : 0;
-    if (other >= sums) zero_behind(zeros, cu, B, N, other - sums);
-    else if (heads.bf16) head_sum<bf16>(heads, cu, B, N, other);
-    else head_sum<float>(heads, cu, B, N, other);
+    T* __restrict__ d_logit, int B, int H, int N, ZeroList zeros, HeadSum heads, PlanOut plan) {
+  if ((int)blockIdx.x >= B * H) {  // what rides on the launch
+    const int other = (int)blockIdx.x - B * H;
+    if constexpr (GRAD) {
+      const int sums = heads.splits > 1 ? kSumGroups : 0;
+      if (other >= sums) zero_behind(zeros, cu, B, N, other - sums);
+      else if (heads.bf16) head_sum<bf16>(heads, cu, B, N, other);
+      else head_sum<float>(heads, cu, B, N, other);
+    } else {
+      plan_or_zeros(plan, zeros, cu, B, N, other);
+    }
     return;
   }
   __shared__ __attribute__((aligned(16))) float row[kPScanSegment];
@@ -246,26 +272,28 @@ __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
   }
 }
 
-int packed_items(int B, int N) { return N / kPackedBlock + std::min(B, N); }
-
 hipError_t launch_packed_plan(const int* cu, int B, int N, void* plan, const ZeroRows* zeros,
                               int n_zeros, hipStream_t s) {
-  const int groups = ((N + kPackedBlock - 1) / kPackedBlock + 3) / 4;  // a wave per block number
-  hipLaunchKernelGGL(packed_plan_kernel, dim3(groups + (n_zeros ? kZeroGroups : 0)), dim3(256), 0, s,
-                     cu, B, N, (PackedItem*)plan, packed_items(B, N), groups,
-                     zero_list(zeros, n_zeros));
+  const PlanOut out = plan_out(plan, B, N, 4);
+  hipLaunchKernelGGL(packed_plan_kernel, dim3(out.groups + (n_zeros ? kZeroGroups : 0)), dim3(256), 0,
+                     s, cu, B, N, out, zero_list(zeros, n_zeros));
   return hipGetLastError();
 }
 
 hipError_t launch_packed_prefix(bool bf16_, const void* logit, const int* cu, float* c, int B,
-                                int H, int N, hipStream_t s) {
-  const dim3 grid((unsigned)B * (unsigned)H), block(kPScanThreads);
+                                int H, int N, void* plan, const ZeroRows* zeros, int n_zeros,
+                                hipStream_t s) {
+  const PlanOut out = plan ? plan_out(plan, B, N, kPScanThreads / 64) : PlanOut{};
+  const dim3 grid((unsigned)B * (unsigned)H + out.groups + (n_zeros ? kZeroGroups : 0)),
+      block(kPScanThreads);
   if (bf16_)
     hipLaunchKernelGGL((packed_scan_kernel<false, bf16>), grid, block, 0, s, nullptr, nullptr,
-                       (const bf16*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{}, HeadSum{});
+                       (const bf16*)logit, cu, c, nullptr, nullptr, B, H, N,
+                       zero_list(zeros, n_zeros), HeadSum{}, out);
   else
     hipLaunchKernelGGL((packed_scan_kernel<false, float>), grid, block, 0, s, nullptr, nullptr,
-                       (const float*)logit, cu, c, nullptr, nullptr, B, H, N, ZeroList{}, HeadSum{});
+                       (const float*)logit, cu, c, nullptr, nullptr, B, H, N,
+                       zero_list(zeros, n_zeros), HeadSum{}, out);
   return hipGetLastError();
 }
 
@@ -279,11 +307,11 @@ hipError_t launch_packed_gate_grad(bool bf16_, const float* dcq, const float* dc
   if (bf16_)
     hipLaunchKernelGGL((packed_scan_kernel<true, bf16>), grid, block, 0, s, dcq, dck,
                        (const bf16*)logit, cu, nullptr, d_log_f, (bf16*)d_logit, B, H, N,
-                       zero_list(zeros, n_zeros), sum);
+                       zero_list(zeros, n_zeros), sum, PlanOut{});
   else
     hipLaunchKernelGGL((packed_scan_kernel<true, float>), grid, block, 0, s, dcq, dck,
                        (const float*)logit, cu, nullptr, d_log_f, (float*)d_logit, B, H, N,
-                       zero_list(zeros, n_zeros), sum);
+                       zero_list(zeros, n_zeros), sum, PlanOut{});
   return hipGetLastError();
 }
 

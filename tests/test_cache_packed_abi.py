@@ -130,6 +130,12 @@ def test_packed_arguments(lib):
     assert plan(p, 1, 10, p, 15, None, 0, None) == WORKSPACE
     assert plan(p, 1, 10, p, 1 << 20, None, 1, None) == NULL
     assert plan(p, 1, 10, p, 1 << 20, None, 9, None) == SHAPE
+    start = lib.fox_packed_start
+    ok = (1, p, p, p, 1, 2, 10, p, 1 << 20, None, 0, None)
+    for i, bad, status in ((1, None, NULL), (2, None, NULL), (3, None, NULL), (7, None, NULL),
+                           (0, 3, UNSUPPORTED), (1, p + 2, ALIGN), (7, p + 8, ALIGN), (8, 15, WORKSPACE),
+                           (5, 0, SHAPE), (6, 0, SHAPE), (10, 9, SHAPE), (10, 1, NULL)):
+        assert start(*ok[:i], bad, *ok[i + 1:]) == status, i
     prefix = lib.fox_gate_prefix_packed
     assert prefix(1, p, None, p, 1, 1, 10, None) == NULL
     assert prefix(1, p, p, p, 1, 0, 10, None) == SHAPE
@@ -190,6 +196,7 @@ def test_bindings_refuse_host_tensors_and_wrong_shapes():
     for call in (lambda: fox.fox_packed_plan(cu, 3),
                  lambda: fox.fox_packed_plan(cu[:1], 3),
                  lambda: fox.fox_gate_prefix_packed(torch.zeros((2, 3)), cu),
+                 lambda: fox.fox_packed_start(torch.zeros((2, 3)), cu),
                  lambda: fox.fox_gate_prefix_packed(torch.zeros((2, 3), dtype=torch.float16), cu),
                  lambda: fox.fox_attn_fwd_packed(*(torch.zeros((2, 3, 64)),) * 3,
                                                  torch.zeros((2, 3)), cu),

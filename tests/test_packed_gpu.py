@@ -134,6 +134,17 @@ def test_prefix_sums(dtype):
         assert ((c[:, cu[b]:cu[b + 1]].double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens", [[1], [0, 0, 5], [3] * 300 + [5000], list(range(0, 700, 7))])
+def test_both_in_one_launch(lens, dtype):
+    """fox_packed_start's list and prefix sums are bit for bit those of the two calls."""
+    _, _, _, _, logit, cu, dcu = _inputs(3, 1, 64, lens, BF, dtype, 6, 4)
+    N = logit.shape[1]
+    plan, c = fox.fox_packed_start(logit, dcu)
+    assert torch.equal(plan, fox.fox_packed_plan(dcu, N))
+    assert torch.equal(c[:, :cu[-1]], fox.fox_gate_prefix_packed(logit, dcu)[:, :cu[-1]])
+
+
 def test_gates_of_every_size():
     """log sigmoid of the smallest to the largest finite logits, each a sequence of its own."""
     x = torch.tensor([0.0, 1e-30, -1e-30, 0.5, -0.5, 17.0, -17.0, 88.0, -88.0, 104.0, -104.0, 1e4, -1e4,
