@@ -238,8 +238,11 @@ __global__ __launch_bounds__(kPScanThreads) void packed_scan_kernel(
       if (lane >= off) incl += y;
     }
     if (lane == 63) wave_total[wave] = incl;
+    // The sum of the lanes before this one, not incl - sum: a term of the lane's own that is
+    // far larger (a gate that forgets everything) or not finite would take them with it.
+    const double lanes = __shfl_up(incl, 1);
     __syncthreads();
-    double prior = carry + (incl - sum);
+    double prior = carry + (lane ? lanes : 0.0);
 #pragma unroll
     for (int w = 0; w < kPScanThreads / 64; ++w) {
       if (w < wave) prior += wave_total[w];
