@@ -145,9 +145,10 @@ static PlanOut plan_out(void* plan, int B, int N, int waves) {  // a wave per bl
 }
 
 // exp(a), a <= 0, on the transcendental unit: the product with log2(e) in two parts, so that large
-// a keep their digits (from -128 on the result is 0, and the parts stay finite).
+// a keep their digits (from -128 on the result is 0, and the parts stay finite).  A NaN stays one
+// (a maximum would take the -128), so that a logit that is none shows in c and the gradients.
 __device__ __forceinline__ float exp_short(float a) {
-  a = fmaxf(a, -128.0f);
+  a = a < -128.0f ? -128.0f : a;
   const float y = a * kLog2e;
   const float lo = __builtin_fmaf(a, kLog2e, -y) + a * 1.9259629e-8f;  // log2(e) - float(log2(e))
   const float e = exp2_fast(y);
