@@ -594,12 +594,12 @@ void attn_cache_kernel(
     }
     const size_t R = ((size_t)b * cv.H + hk * G + g) * n + t;
     if (pc.count == 1) {
-      const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;  // a row without a key: zeros, -inf
+      const float inv = lr == 0.0f ? 0.0f : 1.0f / lr;  // a row without a key: zeros, -inf
       bf16x4 w4;
 #pragma unroll
       for (int j = 0; j < 4; ++j) w4[j] = to_bf16(o[j] * inv);
       *reinterpret_cast<bf16x4*>(O + R * D + e) = w4;
-      if (e == 0) LSE[R] = lr > 0.0f ? kLn2 * (Mr + log2f(lr)) : -INFINITY;
+      if (e == 0) LSE[R] = lr == 0.0f ? -INFINITY : kLn2 * (Mr + log2f(lr));
     } else {
       const size_t at = ((size_t)(pc.first + pc.split) * cv.H + hk * G + g) * n + t;
       *reinterpret_cast<f32x4*>(parts.o + at * D + e) = o;
@@ -854,7 +854,7 @@ void attn_cache_rows_kernel(
     if (!rows.mine[i]) continue;
     const size_t R = rows.out(i, b, cv.H, n);
     if (pc.count == 1) {
-      const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;  // a row without a key: zeros, -inf
+      const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;  // a row without a key: zeros, -inf
 #pragma unroll
       for (int db = 0; db < NB; ++db) {
         bf16x4 w;
@@ -862,7 +862,7 @@ void attn_cache_rows_kernel(
         for (int j = 0; j < 4; ++j) w[j] = to_bf16(oacc[i][db][j] * inv);
         *reinterpret_cast<bf16x4*>(O + R * D + 16 * db + 4 * grp) = w;
       }
-      if (grp == 0) LSE[R] = lt > 0.0f ? kLn2 * (m[i] + log2f(lt)) : -INFINITY;
+      if (grp == 0) LSE[R] = lt == 0.0f ? -INFINITY : kLn2 * (m[i] + log2f(lt));
     } else {
       // (piece, head, token): R without its sequence
       const size_t at = (size_t)(pc.first + pc.split - b) * cv.H * n + R;
@@ -919,12 +919,12 @@ __global__ __launch_bounds__(D / 4 * SG) void attn_cache_join_kernel(
     l = l * a + sml[g][1] * f;
     M = Mn;
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   bf16x4 w;
 #pragma unroll
   for (int j = 0; j < 4; ++j) w[j] = to_bf16(o[j] * inv);
   *reinterpret_cast<bf16x4*>(O + R * D + 4 * part) = w;
-  if (part == 0) LSE[R] = l > 0.0f ? kLn2 * (M + log2f(l)) : -INFINITY;
+  if (part == 0) LSE[R] = l == 0.0f ? -INFINITY : kLn2 * (M + log2f(l));
 }
 
 // ---------------------------------------------------------------------------
