@@ -30,7 +30,8 @@ class PagedCache:
     k_exp, v_exp: [n_pages, H_kv, page] uint8, the scales 2^(exp - 127) of quantised rows;
     c: [n_pages, H, page] fp32, the running sum of log f; page_table: [B, max_pages] int32.
     page is 16, 32, 64, 128 or 256.  The tensors are kept and checked once, here; what they
-    hold, the page table too, may change between calls."""
+    hold, the page table too, may change between calls.  Other tensors (a larger page table)
+    need another PagedCache: the attributes are read-only, and the tensors must not be resized."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, c: torch.Tensor,
                  page_table: torch.Tensor, k_exp: Optional[torch.Tensor] = None,
@@ -50,15 +51,19 @@ class PagedCache:
                 _check(t, name, (n_pages, Hkv, page), torch.uint8, dev)
             elif t is not None:
                 raise ValueError(f"{name} belongs to a float8_e4m3fn cache")
-        self.k, self.v, self.c, self.page_table = k, v, c, page_table
-        self.k_exp, self.v_exp = k_exp, v_exp
-        self.dtype, self.device = k.dtype, dev
-        self.n_pages, self.page, self.max_pages = n_pages, page, max_pages
-        self.B, self.H, self.H_kv, self.d = B, H, Hkv, d
-        self._struct = _CacheStruct(_FORMATS[k.dtype], n_pages, page, max_pages, B, H, Hkv, d,
-                                    _ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), _ptr(c),
-                                    _ptr(page_table))
-        self._ref = ctypes.addressof(self._struct)
+        struct = _CacheStruct(_FORMATS[k.dtype], n_pages, page, max_pages, B, H, Hkv, d, _ptr(k),
+                              _ptr(v), _ptr(k_exp), _ptr(v_exp), _ptr(c), _ptr(page_table))
+        self.__dict__.update(
+            k=k, v=v, c=c, page_table=page_table, k_exp=k_exp, v_exp=v_exp, dtype=k.dtype,
+            device=dev, n_pages=n_pages, page=page, max_pages=max_pages, B=B, H=H, H_kv=Hkv, d=d,
+            _struct=struct, _ref=ctypes.addressof(struct))
+
+    # the calls go by the struct's addresses, so what they stand for stays with them
+    def __setattr__(self, name, value):
+        raise AttributeError(f"PagedCache.{name} is read-only: make another PagedCache")
+
+    def __delattr__(self, name):
+        raise AttributeError(f"PagedCache.{name} is read-only")
 
     @classmethod
     def empty(cls, page_table: torch.Tensor, n_pages: int, heads: int, kv_heads: int, d: int,
