@@ -125,6 +125,19 @@ struct CaSplit {
   int min_units;  // of a piece
   int target;     // pieces wanted; 0: one of each sequence
 };
+// Units of a piece at most, for `total` units of all sequences (2^40 of them where 2^16 tables of
+// 2^30 tokens share pages): never more than a sequence has, so that the number fits, and with it
+// the pieces, of which there are target + B at most.
+constexpr int kCaOnePiece = 1 << 30;
+__host__ __device__ constexpr int ca_most(long long total, const CaSplit& sp) {
+  const long long even = sp.target == 0 ? kCaOnePiece : (total + sp.target - 1) / sp.target;
+  const long long most = even > sp.min_units ? even : sp.min_units;
+  return most < kCaOnePiece ? (int)most : kCaOnePiece;
+}
+static_assert(ca_most(1000, CaSplit{64, 8, 4}) == 250 && ca_most(5, CaSplit{64, 8, 4}) == 8);
+static_assert(ca_most(1LL << 40, CaSplit{64, 8, 1}) == kCaOnePiece);
+static_assert(ca_most((1LL << 32) + 100, CaSplit{64, 8, 1}) == kCaOnePiece);
+static_assert(ca_most(1000, CaSplit{64, 8, 0}) == kCaOnePiece);
 // Piece number `piece`, found by every wave for itself from the lengths of the sequences: with
 // W units of keys in all, a piece has max(min_units, ceil(W / target)) units at most, so that
 // there are at most target + B of them whatever the lengths, and a sequence's pieces are
@@ -148,8 +161,7 @@ __device__ __forceinline__ bool ca_piece(const CacheView& cv, const int* __restr
     for (int off = 32; off > 0; off >>= 1) u += __shfl_xor(u, off);
     total += u;
   }
-  const int most = sp.target == 0 ? 1 << 30
-                                  : (int)max((long long)sp.min_units, (total + sp.target - 1) / sp.target);
+  const int most = ca_most(total, sp);
   int first = 0;
   for (int b0 = 0; b0 < cv.B; b0 += 64) {
     const int u = cv.B <= 64 ? u0 : units_of(b0 + lane), pieces = u / most + (u % most != 0);
