@@ -7,8 +7,8 @@ from typing import Optional, Tuple
 
 import torch
 
-from ._lib import (_DT, _call, _check, _need, _ptr, _raise, _workspace, _workspace_bytes,
-                   default_scale, load)
+from ._lib import (_DT, _call, _check, _check_int, _need, _ptr, _raise, _workspace,
+                   _workspace_bytes, default_scale, load)
 
 FOX_CACHE_BF16 = 0
 FOX_CACHE_E4M3 = 1
@@ -41,6 +41,7 @@ class PagedCache:
         n_pages, Hkv, page, d = k.shape
         H, (B, max_pages) = c.shape[1], page_table.shape
         dev = k.device
+        _check_int(max(n_pages, B, max_pages), "n_pages, B and max_pages")
         _check(k, "k", (n_pages, Hkv, page, d), k.dtype, None)
         _check(v, "v", (n_pages, Hkv, page, d), k.dtype, dev)
         _check(c, "c", (n_pages, H, page), torch.float32, dev)
@@ -131,6 +132,7 @@ def fox_cache_keep(cache: PagedCache, seq_len: torch.Tensor, index: torch.Tensor
     accepted path of a tree of drafts.  index [B,n] (n <= 64), n_keep [B] int32.  seq_len is
     left to the caller, who adds n_keep to it."""
     n, dev = index.shape[1], cache.device
+    _check_int(n, "n")
     _need(seq_len, "seq_len", (cache.B,), torch.int32, dev)
     _need(index, "index", (cache.B, n), torch.int32, dev)
     _need(n_keep, "n_keep", (cache.B,), torch.int32, dev)

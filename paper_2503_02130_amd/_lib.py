@@ -233,6 +233,12 @@ def _need(t, name: str, shape, dtype, device):
         _check(t, name, shape, dtype, device)
 
 
+def _check_int(x: int, name: str):
+    """A size that the C calls take as an int; ctypes would cut a larger one to 32 bits."""
+    if x >= 1 << 31:
+        raise ValueError(f"{name} must be below 2^31 (got {x})")
+
+
 def _check(t: torch.Tensor, name: str, shape, dtype, device):
     """A GPU tensor on `device` (None: any) of this shape and dtype (None: any),
     contiguous; what passes is decided first, what is wrong named after."""

@@ -7,8 +7,8 @@ from typing import Optional, Sequence, Tuple
 
 import torch
 
-from ._lib import (_DT, _call, _check, _need, _ptr, _raise, _workspace, _workspace_bytes,
-                   default_scale, load)
+from ._lib import (_DT, _call, _check, _check_int, _need, _ptr, _raise, _workspace,
+                   _workspace_bytes, default_scale, load)
 
 
 class _RowsStruct(ctypes.Structure):
@@ -49,6 +49,7 @@ def _check_qkv(q, k, v):
 def fox_packed_plan(cu_seqlens: torch.Tensor, N: int) -> torch.Tensor:
     """The work list of a batch of packed sequences (cu_seqlens [B+1] int32, N rows), for
     fox_attn_fwd_packed and fox_attn_bwd_packed of every layer."""
+    _check_int(N, "N")
     B, dev = _check_cu(cu_seqlens, None), cu_seqlens.device
     lib = load()
     places = _plan_places(B, N)
@@ -63,6 +64,7 @@ def fox_gate_prefix_packed(gate_logit: torch.Tensor, cu_seqlens: torch.Tensor,
     """c [H,N] fp32, the running sum of log sigmoid(gate_logit) within each sequence;
     gate_logit [H,N] fp32 or bf16."""
     H, N = gate_logit.shape
+    _check_int(N, "N")
     dt, dev = gate_logit.dtype, gate_logit.device
     if dt not in _DT:
         raise ValueError(f"unsupported dtype {dt}")
@@ -82,6 +84,7 @@ def fox_packed_start(gate_logit: torch.Tensor, cu_seqlens: torch.Tensor
                      ) -> Tuple[torch.Tensor, torch.Tensor]:
     """(plan, c): fox_packed_plan and fox_gate_prefix_packed in one launch."""
     H, N = gate_logit.shape
+    _check_int(N, "N")
     dt, dev = gate_logit.dtype, gate_logit.device
     if dt not in _DT:
         raise ValueError(f"unsupported dtype {dt}")
@@ -186,10 +189,11 @@ def fox_attn_bwd_packed(q, k, v, c, o, lse, d_o, gate_logit: torch.Tensor,
 
 def fox_packed_zero_behind(tensors: Sequence[torch.Tensor], cu_seqlens: torch.Tensor) -> None:
     """Zeros in the rows behind the last sequence of up to 8 packed tensors [heads, N, ...]."""
-    B, dev = _check_cu(cu_seqlens, None), cu_seqlens.device
     if not 1 <= len(tensors) <= 8:
         raise ValueError(f"1 to 8 tensors (got {len(tensors)})")
     N = tensors[0].shape[1]
+    _check_int(N, "N")
+    B, dev = _check_cu(cu_seqlens, None), cu_seqlens.device
     rows = (_RowsStruct * len(tensors))()
     for i, t in enumerate(tensors):
         _need(t, f"tensors[{i}]", (t.shape[0], N, *t.shape[2:]), None, dev)

@@ -1,5 +1,7 @@
-"""The bindings of the cache and the packed calls, on the host: what they hold on to."""
+"""The bindings of the cache and the packed calls, on the host: what they hold on to and what
+they refuse before any call."""
 import pytest
+import torch
 
 import paper_2503_02130_amd as fox
 
@@ -20,3 +22,28 @@ def test_a_cache_is_set_once(name):
     with pytest.raises(AttributeError):
         delattr(cache, name)
     assert getattr(cache, name) == 1
+
+
+WIDE = (1 << 32) + 128  # 128 as a 32-bit number
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """The C calls take ints, which ctypes cuts to 32 bits: such a call would do a part of the
+    work, or go by other strides, and report success."""
+    logit = torch.empty((1, WIDE), device="meta")
+    cu = torch.zeros((2,), dtype=torch.int32)
+    rows = torch.empty((1, WIDE, 2), device="meta")
+    for call in (lambda: fox.fox_packed_plan(cu, WIDE), lambda: fox.fox_gate_prefix_packed(logit, cu),
+                 lambda: fox.fox_packed_start(logit, cu),
+                 lambda: fox.fox_packed_zero_behind([rows], cu)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+    k = torch.empty((8, 2, 64, 128), device="meta", dtype=torch.bfloat16)
+    c, table = (torch.empty(s, device="meta", dtype=t) for s, t in (
+        ((8, 4, 64), torch.float32), ((1, WIDE), torch.int32)))
+    with pytest.raises(ValueError, match="2\\^31"):
+        fox.PagedCache(k, k, c, table)
+    cache = object.__new__(fox.PagedCache)
+    cache.__dict__.update(B=1, device=torch.device("cuda", 0))
+    with pytest.raises(ValueError, match="2\\^31"):
+        fox.fox_cache_keep(cache, cu, torch.empty((1, WIDE), device="meta", dtype=torch.int32), cu)
