@@ -69,7 +69,8 @@ typedef enum {
   FOX_ERR_ALIGN = 4,        /* a pointer is not 16-byte aligned                    */
   FOX_ERR_WORKSPACE = 5,    /* workspace missing or smaller than required          */
   FOX_ERR_HIP = 6,          /* the HIP runtime reported an error at launch         */
-  FOX_ERR_VALUE = 7,        /* a scalar argument out of range (eps: finite, >= 0)  */
+  FOX_ERR_VALUE = 7,        /* a scalar argument out of range (eps: finite, >= 0;
+                               scale of packed bf16 calls)                         */
   FOX_ERR_TOO_LARGE = 8,    /* the shape needs more scratch than the allocation-free
                                entry point holds                                   */
   FOX_STATUS_MAX_ENUM = 0x7FFFFFFF  /* not a status: keeps the enum int-sized        */
@@ -529,6 +530,7 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  *                  sequence hold does not matter; they are not written except to set them
  *                  to zero.
  *   N * H and the rows of a head in bytes must be below 2^31.
+ *   scale: in bf16 finite and at least 2^-64 in magnitude (else FOX_ERR_VALUE).
  *
  * fox_packed_plan: the list of 128-row blocks that the attention calls walk, the heaviest
  *   first, into a device buffer of fox_packed_plan_bytes(); made once for a batch (its

@@ -115,6 +115,11 @@ fox_status_t check_packed(int B, int H, int H_kv, int N) {
   return FOX_OK;
 }
 
+// The bf16 kernels hold (c_i - c_j) / scale in fp32.
+bool packed_scale_ok(int dtype, float scale) {
+  return dtype != FOX_DTYPE_BF16 || (isfinite(scale) && fabsf(scale) >= 0x1p-64f);
+}
+
 fox_status_t zero_rows(const fox_packed_rows_t* tensors, int n, fox::ZeroRows* x) {
   if (n < 0 || n > fox::kZeroTensors) return FOX_ERR_SHAPE;
   if (n > 0 && !tensors) return FOX_ERR_NULL;
@@ -1006,6 +1011,7 @@ fox_status_t fox_attn_fwd_packed(fox_dtype_t dtype, const void* q, const void* k
   st = check_dtype_d(dtype, d);
   if (st) return st;
   if (o_lo && dtype != FOX_DTYPE_BF16) return FOX_ERR_UNSUPPORTED;
+  if (!packed_scale_ok(dtype, scale)) return FOX_ERR_VALUE;
   if (!all_aligned16({q, k, v, c, plan, o, o_lo, lse})) return FOX_ERR_ALIGN;
   const int len = max_len <= 0 || max_len > N ? N : max_len;
   if (dtype == FOX_DTYPE_BF16)
@@ -1040,6 +1046,7 @@ fox_status_t fox_attn_bwd_packed(fox_dtype_t dtype, const void* q, const void* k
   st = check_dtype_d(dtype, d);
   if (st) return st;
   if (!cache_dtype(gate_dtype) || (o_lo && dtype != FOX_DTYPE_BF16)) return FOX_ERR_UNSUPPORTED;
+  if (!packed_scale_ok(dtype, scale)) return FOX_ERR_VALUE;
   if (!all_aligned16({q, k, v, c, o, o_lo, lse, d_o, gate_logit, cu_seqlens, plan, dq, dk, dv, d_logit,
                       d_log_f, workspace}))
     return FOX_ERR_ALIGN;

@@ -47,3 +47,26 @@ def test_sizes_beyond_32_bits_are_refused():
     cache.__dict__.update(B=1, device=torch.device("cuda", 0))
     with pytest.raises(ValueError, match="2\\^31"):
         fox.fox_cache_keep(cache, cu, torch.empty((1, WIDE), device="meta", dtype=torch.int32), cu)
+
+
+@pytest.mark.parametrize("scale,good", [(0.0, False), (-0.0, False), (2.0 ** -65, False),
+                                        (float("inf"), False), (float("nan"), False),
+                                        (2.0 ** -64, True), (-0.125, True)])
+def test_bf16_packed_attention_needs_a_scale_to_divide_by(scale, good):
+    """Its kernels hold (c_i - c_j) / scale; fp32's do not.  A missing workspace or o_lo of an fp32
+    o is refused after the scale, so nothing is launched."""
+    p, lib = 0x10000, fox.load()
+    value, unsupported, workspace, align = 7, 3, 5, 4
+
+    def fwd(dtype, o=p, o_lo=None):
+        return lib.fox_attn_fwd_packed(dtype, p, p, p, p, p, o, o_lo, p, 1, 4, 2, 100, 64, 0, scale,
+                                       None)
+
+    def bwd(dtype, o_lo=None):
+        return lib.fox_attn_bwd_packed(dtype, *(p,) * 5, o_lo, p, p, 0, *(p,) * 7, None, 0, None, 0,
+                                       1, 4, 2, 100, 64, 0, scale, None)
+
+    assert fwd(1, o=p + 4) == (align if good else value)
+    assert bwd(1) == (workspace if good else value)
+    assert fwd(0, o_lo=p) == unsupported and bwd(0, o_lo=p) == unsupported
+    assert fwd(0, o=p + 4) == align and bwd(0) == workspace
