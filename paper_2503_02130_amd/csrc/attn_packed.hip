@@ -164,7 +164,7 @@ void packed_fwd_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
   };
   auto store_c = [&](auto bufc) {
     constexpr int B = decltype(bufc)::value;
-    if (wave == 0) sm.c[B][lane] = ckey < L ? (c_q0 - craw) * inv_scale : -INFINITY;
+    if (wave == 0) sm.c[B][lane] = (ckey < L ? c_q0 - craw : -INFINITY) * inv_scale;
   };
   auto max32 = [&](const float* u) {
     float mt = u[0];
@@ -567,7 +567,7 @@ void packed_dq_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
     constexpr bool MASK = decltype(masked)::value;
     const int key0 = j * kPkBN;
     const float dref = cq - *(const lds_f32_t*)(cref_at + 4 * B);
-    const float bq = q_valid ? (dref - lse_q) * inv_scale : -INFINITY;
+    const float bq = (q_valid ? dref - lse_q : -INFINITY) * inv_scale;
     static_for<2>([&](auto kbc) {
       constexpr int kb = decltype(kbc)::value;
       f32x16 sacc, pacc;
@@ -840,8 +840,9 @@ void packed_dkdv_kernel(const bf16* __restrict__ Q, const bf16* __restrict__ K,
     constexpr int B = decltype(bufc)::value;
     if (wave == 0 && lane < BM) {
       const int qq = (t_first + x.t) * BM + lane;
-      sm.bq[B][lane] = qq < L ? ((sm.raw[rb][0][lane] - conv_ck0) - sm.raw[rb][1][lane]) * inv_scale
-                              : -INFINITY;
+      // (behind the sequence the infinity that the scale, of either sign, turns into -infinity)
+      sm.bq[B][lane] = (qq < L ? (sm.raw[rb][0][lane] - conv_ck0) - sm.raw[rb][1][lane] : -INFINITY) *
+                       inv_scale;
       sm.dl[B][lane] = qq < L ? sm.raw[rb][2][lane] : 0.0f;
     }
   };
