@@ -9,8 +9,10 @@
 //
 // with k~, v~ the codes and 2^ek, 2^ev the rows' scales (1 for a bf16 cache).  A lane holds codes
 // of one key, whose scale the conversion to bf16 applies (exact; keys whose values are below
-// 2^-117 may lose digits that no score sees).  V's scale multiplies a weight, and its codes
-// go to the matrix cores unscaled.
+// 2^-117 may lose digits that no score sees).  V's scale multiplies a weight before it is
+// rounded to bf16, and its codes go to the matrix cores unscaled: a product below 2^-126 may
+// vanish, 2^-29 of the largest weight in a row of 2^-90.  Weights reach 2^8 before a rescale, so
+// sums over values above 2^100 may overflow (in a bf16 cache too).
 //
 //   * The G n rows of a key head share its keys: rows are r = g n + t, 16 to a tile.  Two
 //     kernels: up to 16 rows (e4m3: 32 or 64) the four waves of a workgroup split the keys of one
@@ -43,9 +45,11 @@
 // plain copy of this part reaches 4.8 and a streaming read 6.6.  A single short sequence is
 // launch and latency: 2047 tokens, H = 12, d = 64 6.8 us and 2.6 to join.  Trees: 16 drafts of 16 bf16
 // sequences of 100 to 8 thousand tokens 29 us at 5.5 TB/s (and 6 to join); 64 drafts of four e4m3
-// sequences of 3 to 16 thousand, H = 16, H_kv = 2 46 us, VALU: 7.8 vector instructions to a matrix
-// instruction (the conversion of the codes, the exponentials, the weights' scales), matrix
-// cores busy a third of the time.
+// sequences of 3 to 16 thousand, H = 16, H_kv = 2 45 us (and 8 to join): 7.8 vector instructions to
+// a matrix instruction (the conversion of the codes, which every wave does for itself, the
+// exponentials, the weights' scales), which one after the other would take 63% of its cycles
+// (matrix 22%); the rest is the wait for tiles and barriers (23% of the waves' cycles), starts and
+// ends: a workgroup has about ten tiles.
 #include <algorithm>
 
 #include "fox_internal.h"
@@ -963,8 +967,9 @@ constexpr long long kCaWant = 2048, kCrWant2 = 512, kCrWant3 = 768;
 // 19.0; 128 of 1000 37.4 / 32.4 / 26.3 (not split).  Sharing, 1024 leaves CUs idle where the
 // lengths differ: 64 drafts of four sequences of 3 to 16 thousand tokens 51 / 51 / 66.
 constexpr long long kCaSome = 80000, kCaMany = 500000;
-// Bytes of K and V from which they bypass the caches when one row block reads them: 1.5 times
-// the 256 MB that the last level holds.  us with / without: e4m3, d = 128, 64 sequences of 20000
+// Bytes of K and V from which they bypass the caches when one row block of up to 64 rows reads
+// them: 1.5 times the 256 MB that the last level holds.  Two row tiles to a wave (65 to 128 rows)
+// go through the caches, whatever their size (the other way was not measured).  us with / without: e4m3, d = 128, 64 sequences of 20000
 // (1.3 GB) 213 / 248, 32 of 8000 (262 MB, in the cache from the call before) 56 / 51; bf16 64 of
 // 20000 425 / 462, 32 of 8000 97 / 106.
 constexpr long long kCaBypass = 384LL << 20;
@@ -985,7 +990,7 @@ static CaPlan ca_plan(const CacheSpec& s, int n, int max_len) {
   p.rt = p.shared && rows > 64 && seqs * blocks(2) * max_len >= kCrTwo ? 2 : 1;
   p.n_rowblk = p.shared ? blocks(p.rt) : (rows + 15) / 16;
   const long long all = seqs * p.n_rowblk * max_len;  // keys of all workgroups, at most
-  p.once = p.n_rowblk == 1 && large;
+  p.once = p.n_rowblk == 1 && p.rt == 1 && large;
   const int least = all < kCaSome ? 256 : all < kCaMany || p.shared ? 512 : 1024;
   const long long want = !p.shared ? kCaWant : p.rt == 2 || (s.d == 128 && !s.f8) ? kCrWant2 : kCrWant3;
   p.split.unit = p.shared ? kCrTile : kCaRound;
