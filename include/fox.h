@@ -520,7 +520,8 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
 /*
  * Packed sequences with grouped heads: B sequences of different lengths, one behind the
  * other, without padding.  Query head h reads key head h / (H / H_kv) and has its own forget
- * gate; H is a multiple of H_kv.
+ * gate; H is a multiple of H_kv.  (fox_pro_prologue knows no cu_seqlens: on packed rows its KV
+ * shift would carry from one sequence to the next.)
  *
  *   q, o, o_lo, d_o, dq  [H,N,d] dtype     k, v, dk, dv  [H_kv,N,d] dtype
  *   gate logits    [H,N] fp32 or bf16 (gate_dtype)     c, lse [H,N] fp32
@@ -538,10 +539,15 @@ fox_status_t fox_gate_projection_bwd(fox_dtype_t dtype, const void* x, const flo
  *   does for them what fox_packed_zero_behind does, in the same launch (n = 0: tensors may be
  *   NULL).  Blocks of a list that do not lie within a call's N rows are skipped.
  * fox_gate_prefix_packed: c, the running sum of log sigmoid(gate_logit) within each sequence
- *   (summed in 64 bits, rounded once).
+ *   (summed in 64 bits, rounded once: behind a c of -2^24, steps of less than 1 are lost).
  * fox_packed_start: fox_packed_plan and fox_gate_prefix_packed in one launch.
  * fox_attn_fwd_packed: O and LSE of each sequence as fox_attn_fwd's.  max_len: the longest
  *   sequence, if known, else 0 (N): it decides how the work is split, not what is computed.
+ *   Short sequences want it: with 0 their backward is split as one sequence of N rows would be
+ *   (a step of 40 of 256 rows, H = 12, H_kv = 4, d = 64, 102 us in place of 88 and 64 MB of
+ *   workspace in place of 1.5; of 100 of 100 rows, H = 8, H_kv = 2, d = 128, 137 for 97, 83 MB for 1).
+ *   The error of a score and of LSE in bf16 is 1e-6, more where c falls by much over 128 rows (up
+ *   to about 2^-20 of the fall; 1.6e-4 seen for 528).
  *   o_lo (bf16, may be NULL): what rounding took from o, for the backward.
  * fox_attn_bwd_packed: the gradients of sum(O o dO): dq, dk, dv (dk, dv summed over the query
  *   heads of a key head) and d_logit in gate_dtype, the gradient of the gate logits; d_log_f
@@ -631,7 +637,8 @@ typedef struct {
  *     parent      [B,n] int32  in   the new token that a new token follows, less than its own
  *                 number; negative (or not less): the last cached token.  NULL: a chain.
  *     n_new       [B]   int32  in   how many of the n a sequence has; NULL: all
- *   c of a token is c of the token that it follows plus log sigmoid(gate_logit).  Values that
+ *   c of a token is c of the token that it follows (0 if that one has no page) plus
+ *   log sigmoid(gate_logit).  Values that
  *   are not finite become NaN in an E4M3 cache and do not take part in the row's scale.
  * fox_cache_append_packed: writes whole prompts, packed as for fox_attn_fwd_packed, behind
  *   the seq_len[b] cached tokens (NULL: into empty caches).  c [H,N] fp32 comes from
@@ -674,9 +681,11 @@ fox_status_t fox_cache_read(const fox_cache_t* cache, fox_dtype_t dtype, const i
  *           slower.  0: max_pages * page.
  *   workspace  at least fox_attn_cache_workspace_bytes() for the same n and max_len (which
  *           may be 0: then workspace may be NULL)
- * k and v of the tokens in the cache must be finite.  A sequence's keys are split into parts by
- * the shape, max_len and the lengths of all sequences, so its results in another batch agree to
- * rounding; the same call gives the same bits.
+ * k and v of the tokens in the cache must be finite, and v between 2^-90 and 2^100 in magnitude
+ * keeps its accuracy (smaller rows of an E4M3 cache lose small weights, sums of larger values may
+ * overflow).  A NaN in q or c gives o = lse = NaN in the rows that see it.  A sequence's keys are
+ * split into parts by the shape, max_len and the lengths of all sequences, so its results in
+ * another batch agree to rounding; the same call gives the same bits.
  */
 size_t fox_attn_cache_workspace_bytes(const fox_cache_t* cache, int n, int max_len);
 fox_status_t fox_attn_cache(const fox_cache_t* cache, const void* q, const int* seq_len,

@@ -86,7 +86,8 @@ def forgetting_attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     q: [H, N, d], k, v: [H_kv, N, d] bf16 or fp32 on the GPU (d = 64 or 128, H a multiple of
     H_kv); gate_logit: [H, N] fp32 or bf16; cu_seqlens: [B + 1] int32, sequence b being rows
     cu_seqlens[b] .. cu_seqlens[b + 1] - 1.  max_len: the longest sequence, if known (it sets
-    how the work is split).  plan: fox_packed_plan(cu_seqlens, N), to share it between layers.
+    how the work is split; without it batches of short sequences are slower and take a workspace
+    of fp32 partial sums).  plan: fox_packed_plan(cu_seqlens, N), to share it between layers.
     The output and the gradients are zero in rows behind the last sequence.  bf16: a tensor of
     o's size is kept besides o (what rounding took from it) for dq.
 

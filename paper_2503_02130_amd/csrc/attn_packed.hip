@@ -18,8 +18,11 @@
 //     such walk would decide the time, the heads are split over workgroups whose fp32 partial
 //     sums are added up afterwards (packed_head_split).  dc^k, which belongs to a query head,
 //     is written as each head ends.
-//   * The row sum l adds the unrounded fp32 P, so that LSE is an fp32 quantity to its last
-//     digits.  The dQ kernel forms Delta itself from the rows of O and dO that it owns.  The
+//   * The row sum l adds the unrounded fp32 P, so that LSE has fp32 errors only, those of its
+//     scores: 1e-6 where gates hold on, more where a 128-row block forgets much, since the
+//     accumulators start from (c_q0 - c_j) / s and are rounded at that size in each step:
+//     2.5e-5, 1.6e-4 and 1.2e-3 for a c that falls by 111, 528 and 3827 over a block (d = 128; at
+//     most about 2^-24 (d / 16 + 8) of the fall).  The dQ kernel forms Delta itself from the rows of O and dO that it owns.  The
 //     backward forms dS from P rounded to fp16 (2^-12 of it; carried as 2^15 P,
 //     which fp16 holds to full precision down to 2^-29) and dc^k adds the unrounded fp32 dS.
 //   * c_i shifts a whole softmax row, so dc^q = rowsum(dS) is 0; what it comes out as is the
@@ -30,11 +33,15 @@
 //     rows of dS that sum to 0 to fp32 rounding, and d(log f) is the reverse sum of dc^k
 //     alone.  bf16 rounding is left in the operands dS and, for dV, P.
 //
-// Bound by instruction issue, as the dense kernels (matrix and vector instructions overlap in
-// part).  Prompts of 1001 to 8192 tokens, H = 16, H_kv = 4, D = 128: forward 440 us, 1.05 PFLOP/s of
-// a large library product's 1.36.  Three of 1500 to 8191: forward 394, dQ 568, dK/dV 835 us (965,
-// 1000 and 910 TFLOP/s).  Twelve of 64 to 2048, H = 12, D = 64: 52, 73 and 98 us (540, 570, 570): short
-// rows end in masked tiles and D = 64 has half the matrix work to the same exponentials.
+// Forward and dQ at D = 128 are bound by instruction issue, as the dense kernels: one after the
+// other, the instructions would take 81 to 92% of their busy cycles (matrix instructions 53%, and
+// the two kinds overlap in part).  dK/dV, at one workgroup per CU, is at 72% and waits 38% of its
+// waves' cycles for barriers and LDS.  D = 64 (forward 71, dQ 82, dK/dV 67%) has half the matrix
+// work to the same exponentials, short rows that end in masked tiles, and waits 31, 35 and 45%; dK/dV
+// has a barrier for every 32 queries.  Prompts of 1001 to 8192 tokens, H = 16, H_kv = 4, D = 128:
+// 433 us with prefix and plan (12), 1.07 PFLOP/s of a large library product's 1.36.  Three of 1500 to
+// 8191: forward 389, dQ 565, dK/dV 831 us (980, 1010 and 915 TFLOP/s).  Twelve of 64 to 2048, H = 12,
+// D = 64: 51, 73 and 97 us (540, 570, 575).
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>

@@ -146,7 +146,8 @@ const char* fox_status_string(fox_status_t status) {
     case FOX_ERR_ALIGN: return "FOX_ERR_ALIGN: device pointers must be 16-byte aligned";
     case FOX_ERR_WORKSPACE: return "FOX_ERR_WORKSPACE: workspace missing or too small";
     case FOX_ERR_HIP: return "FOX_ERR_HIP: the HIP runtime reported a launch error";
-    case FOX_ERR_VALUE: return "FOX_ERR_VALUE: a scalar argument is out of range (eps: finite, >= 0)";
+    case FOX_ERR_VALUE: return "FOX_ERR_VALUE: a scalar argument is out of range (eps: finite, >= 0; scale of a "
+                                "packed bf16 call: finite, at least 2^-64 in magnitude)";
     case FOX_ERR_TOO_LARGE:
       return "FOX_ERR_TOO_LARGE: the shape needs more scratch than fox_attn_decode_noalloc holds "
              "(64 MiB of split partials); use fox_attn_decode with a workspace";

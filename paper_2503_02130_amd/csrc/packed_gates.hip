@@ -13,7 +13,7 @@
 // The scans run in 64 bits and round once: c of a long sequence is thousands with
 // differences of neighbours that matter, and fp32 sums of it are several units off.  They
 // are short chains of a few barriers per 8192 rows, bound by latency: sequences of up to 8191
-// rows take 6 us, their gradient 12, the plan 4.  What does not depend on a scan rides on its
+// rows take 7 us, their gradient 12, the plan 4 to 5.  What does not depend on a scan rides on its
 // launch: the plan on the prefix's, the sums of split heads (24 us alone beside these 12: 27
 // together) and the zeros behind the last sequence on the gradient's.
 #include <algorithm>
