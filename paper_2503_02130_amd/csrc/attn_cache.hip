@@ -969,9 +969,9 @@ constexpr long long kCaWant = 2048, kCrWant2 = 512, kCrWant3 = 768;
 constexpr long long kCaSome = 80000, kCaMany = 500000;
 // Bytes of K and V from which they bypass the caches when one row block of up to 64 rows reads
 // them: 1.5 times the 256 MB that the last level holds.  Two row tiles to a wave (65 to 128 rows)
-// go through the caches, whatever their size (the other way was not measured).  us with / without: e4m3, d = 128, 64 sequences of 20000
-// (1.3 GB) 213 / 248, 32 of 8000 (262 MB, in the cache from the call before) 56 / 51; bf16 64 of
-// 20000 425 / 462, 32 of 8000 97 / 106.
+// go through the caches, whatever their size (the other way was not measured).  us with / without:
+// e4m3, d = 128, 64 sequences of 20000 (1.3 GB) 213 / 248, 32 of 8000 (262 MB, in the cache from the
+// call before) 56 / 51; bf16 64 of 20000 425 / 462, 32 of 8000 97 / 106.
 constexpr long long kCaBypass = 384LL << 20;
 
 struct CaPlan {
